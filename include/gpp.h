@@ -57,7 +57,7 @@ typedef enum {
   GPP_ERR_UNSUPPORTED = 4, /* valid graph this library has no kernel for (e.g. dtype mix) */
   GPP_ERR_WORKSPACE = 5,   /* workspace too small or misaligned */
   GPP_ERR_ORDER = 6,       /* ordering condition C4 violated, or slot busy / free */
-  GPP_ERR_INDEX = 7,       /* an embedding index, a bag offset or a class label was out of range (see gpp_stage_sync_status) */
+  GPP_ERR_INDEX = 7,       /* an embedding index, a bag offset, a class label or a sample's length was out of range (see gpp_stage_sync_status) */
   GPP_ERR_DEVICE = 8       /* a HIP call failed, see gpp_last_error */
 } gpp_status_t;
 
@@ -83,32 +83,77 @@ typedef enum {
   GPP_OP_LOSS_MSE = 9,      /* in = (prediction, target f32); L = loss_scale * sum (y-t)^2 */
   GPP_OP_LOSS_CE = 10,      /* in = (logits, labels i32 [b,1]); L = -loss_scale * sum log softmax(y)[label] */
   GPP_OP_LOSS_BCE_LOGITS = 11, /* in = (logits, targets f32); L = loss_scale * sum softplus(y) - t*y */
-  GPP_OP_EMBEDDING_BAG_CONCAT = 12 /* producers as EMBEDDING_BAG_SUM; the rows of a bag are concatenated (the
+  GPP_OP_EMBEDDING_BAG_CONCAT = 12, /* producers as EMBEDDING_BAG_SUM; the rows of a bag are concatenated (the
                                    paper's DLRM, appendix "DNN Model Configurations"): in_features = row width d,
                                    out_features = bag_size * d (a multiple of 64),
                                    out[s, j*d:(j+1)*d] = table[idx[off[s] + j], :], zero for j >= the bag's length */
+  GPP_OP_ROTARY = 13,       /* rotary positions with one to four axes (time, height, width, ...).  in[0] = x, in[1] = positions
+                               input (i32, [rows of x, axes]; any values).  The first `heads` blocks of `head_dim` columns are
+                               rotated (the Q and K blocks of a packed Q|K|V row), every other column is handed on unchanged.
+                               Axis a owns axis_pairs[a] pairs of columns, in order; P is their sum, 2 P <= head_dim, and the
+                               last head_dim - 2 P columns of a block are not rotated.  Pair i, the j-th of axis a, turns by
+                               position[a] * w radians: (x0, x1) -> (x0 cos - x1 sin, x0 sin + x1 cos), w = base^(-i/P) on one
+                               ladder of frequencies, base^(-j/axis_pairs[a]) on a ladder per axis.  Angles are formed and
+                               reduced in 64 bits.  out_features = features of x; the output has x's dtype */
+  GPP_OP_ATTENTION_WINDOW = 14 /* attention inside a window, with first tokens that stay visible.  in[0] = [b*S, (heads +
+                               2*kv_heads)*head_dim] as Q|K|V column blocks; query head h reads key / value head
+                               h / (heads / kv_heads).  Query i of a sample sees key j when (not causal or j <= i) and
+                               (window == 0 or |i - j| < window or j < sinks).  in[1], optional: lengths input (i32, [b, 1], 0 to
+                               S each); rows of a sample at and behind its length are padding: not read, output and
+                               gradients zero.  out_features = heads*head_dim, S = seq_len.  The values of rows that are not
+                               padding have to be finite: a key's NaN or infinity may reach queries that do not see it */
 } gpp_op_kind_t;
+
+/* GPP_OP_ROTARY: which columns of a head form pair i */
+typedef enum { GPP_PAIR_HALVES = 0 /* i and P + i */, GPP_PAIR_NEIGHBOURS = 1 /* 2 i and 2 i + 1 */ } gpp_pairing_t;
+/* GPP_OP_ROTARY: the frequencies of its pairs */
+typedef enum { GPP_LADDER_SHARED = 0, GPP_LADDER_PER_AXIS = 1 } gpp_ladder_t;
 
 typedef enum { GPP_ACT_NONE = 0, GPP_ACT_RELU = 1, GPP_ACT_GELU_ERF = 2 } gpp_act_t;
 
 /* One vertex of G_i.  `in` lists producer op ids (the edges E_C inside the
- * stage).  HOST memory; the library copies what it needs during create. */
+ * stage).  HOST memory; the library copies what it needs during create.
+ * Members of a union are names of one field that different operators give different meanings. */
 typedef struct {
   int32_t kind;          /* gpp_op_kind_t */
   int32_t n_in;
   const int32_t *in;     /* HOST, n_in producer ids */
   int32_t branch;        /* branch label (>= 0), -1 for merge / tail operators; informational */
-  int64_t in_features;   /* LINEAR: K; DOT_INTERACT: vector width d */
+  union {
+    int64_t in_features; /* LINEAR: K; DOT_INTERACT: vector width d */
+    int64_t head_dim;    /* ROTARY, ATTENTION_WINDOW: columns of a head */
+  };
   int64_t out_features;  /* feature count of the output (INPUT: of the tensor itself) */
-  int32_t act;           /* gpp_act_t, LINEAR only */
-  int32_t has_bias;      /* LINEAR only */
-  int32_t heads;         /* ATTENTION */
+  union {
+    int32_t act;         /* LINEAR: gpp_act_t */
+    int32_t pairing;     /* ROTARY: gpp_pairing_t */
+  };
+  union {
+    int32_t has_bias;    /* LINEAR */
+    int32_t ladder;      /* ROTARY: gpp_ladder_t */
+    int32_t causal;      /* ATTENTION_WINDOW: 1 = a query sees no key behind itself */
+  };
+  int32_t heads;         /* ATTENTION, ATTENTION_WINDOW: query heads; ROTARY: rotated column blocks */
   int32_t seq_len;       /* rows per sample of the output (INPUT, LAYERNORM, ATTENTION, ...: S; 1 = plain) */
-  int32_t rows_extra;    /* INPUT only: extra rows beyond micro_batch*seq_len (1 for bag offsets) */
+  union {
+    int32_t rows_extra;  /* INPUT: extra rows beyond micro_batch*seq_len (1 for bag offsets) */
+    int32_t kv_heads;    /* ATTENTION_WINDOW: key / value heads, a divisor of heads */
+  };
   int32_t requires_grad; /* INPUT only: 1 = float tensor from a predecessor stage whose gradient is returned */
-  int64_t num_rows;      /* EMBEDDING_BAG_SUM: table rows */
-  int64_t bag_size;      /* EMBEDDING_BAG_SUM: maximum indices per bag (capacity b*bag_size) */
-  double eps;            /* LAYERNORM */
+  union {
+    int64_t num_rows;    /* EMBEDDING_BAG_SUM: table rows */
+    int64_t window;      /* ATTENTION_WINDOW: 0 = no limit */
+    int16_t axis_pairs[4]; /* ROTARY: pairs of each axis; axes that are not there hold 0 and come last */
+  };
+  union {
+    int64_t bag_size;    /* EMBEDDING_BAG_SUM: maximum indices per bag (capacity b*bag_size) */
+    int64_t sinks;       /* ATTENTION_WINDOW: first tokens that every query sees (causal: every later one) */
+  };
+  union {
+    double eps;          /* LAYERNORM */
+    double base;         /* ROTARY: base of the frequencies, above 0 */
+    double scale;        /* ATTENTION_WINDOW: factor of the scores; 0 = 1/sqrt(head_dim) */
+  };
   double loss_scale;     /* LOSS_*: carries the 1/B normalisation of the whole mini-batch, so that
                             micro-batch gradients sum to the full-batch gradient */
   int32_t dtype;         /* gpp_dtype_t of the output tensor as stored */
@@ -235,8 +280,9 @@ gpp_status_t gpp_stage_grad_reset(gpp_stage_t *stage, void *hip_stream);
 
 /* Waits for the stream and reports GPP_ERR_INDEX if any kernel since the last call met an embedding
  * index out of range, bag offsets that break their contract (first offset not 0, decreasing, beyond the
- * capacity) or a class label outside [0, classes) (such entries are skipped, never dereferenced; the
- * results of that micro-batch are then not those of the operator graph). */
+ * capacity), a class label outside [0, classes) (such entries are skipped, never dereferenced; the
+ * results of that micro-batch are then not those of the operator graph) or a length outside [0, seq_len]
+ * (taken as the nearer end). */
 gpp_status_t gpp_stage_sync_status(gpp_stage_t *stage, void *hip_stream);
 
 gpp_status_t gpp_stage_destroy(gpp_stage_t *stage);

@@ -159,6 +159,94 @@ def attention_bwd(do, saved, op, b):
     return [out]
 
 
+def rotary_angles(pos, op):
+    """Angle of every row's pairs: pair i, the j-th of axis a, turns by position[a] * w with w = base^(-i/P)
+    on one ladder of frequencies over all P pairs, base^(-j/P_a) on a ladder per axis."""
+    pairs = [int(p) for p in op["axis_pairs"] if p]
+    total = sum(pairs)
+    cols = []
+    for a, n in enumerate(pairs):
+        for j in range(n):
+            e = j / n if op.get("ladder", "shared") == "per_axis" else len(cols) / total
+            cols.append(pos[:, a].astype(np.float64) * op["base"] ** (-e))
+    return np.stack(cols, axis=1)
+
+
+def _turn(x, angle, op):
+    n, dh, p = op["heads"], op["head_dim"], angle.shape[1]
+    y = x.copy()
+    c, s = np.cos(angle), np.sin(angle)
+    for h in range(n):
+        for i in range(p):
+            i0, i1 = (2 * i, 2 * i + 1) if op.get("pairing", "halves") == "neighbours" else (i, p + i)
+            a, b = x[:, h * dh + i0], x[:, h * dh + i1]
+            y[:, h * dh + i0] = a * c[:, i] - b * s[:, i]
+            y[:, h * dh + i1] = a * s[:, i] + b * c[:, i]
+    return y
+
+
+def rotary_fwd(x, pos, op):
+    """Rotary positions: the first `heads` blocks of head_dim columns turn pair by pair by the angles of the
+    row's positions (time, height, width, ...); every other column is handed on."""
+    angle = rotary_angles(pos, op)
+    return _turn(x, angle, op), angle
+
+
+def rotary_bwd(dy, angle, op):
+    """A rotation's transpose is the rotation by the negative angle; positions have no gradient."""
+    return [_turn(dy, -angle, op)]
+
+
+def window_mask(n, op):
+    """[n, n] truth values: query i (row) sees key j (column) when (not causal or j <= i) and
+    (window == 0 or |i - j| < window or j < sinks)."""
+    i, j = np.arange(n)[:, None], np.arange(n)[None, :]
+    w = op.get("window", 0)
+    seen = np.ones((n, n), bool) if not w else (np.abs(i - j) < w) | (j < op.get("sinks", 0))
+    return seen & (j <= i) if op.get("causal", False) else seen
+
+
+def attention_window_fwd(qkv, lengths, op, b):
+    """Softmax attention over the visible keys; query head h reads key / value head h // (heads / kv_heads);
+    rows at and behind a sample's length are padding: output zero, values not looked at."""
+    s, hq, hk, dh = op["seq_len"], op["heads"], op["kv_heads"], op["head_dim"]
+    scale = op.get("scale", 0.0) or 1.0 / math.sqrt(dh)
+    out = np.zeros((b * s, hq * dh))
+    saved = []
+    for k in range(b):
+        n = s if lengths is None else int(lengths.reshape(-1)[k])
+        if n < 0 or n > s:
+            raise IndexError("length out of range")
+        rows = slice(k * s, k * s + n)
+        seen = window_mask(n, op)
+        for h in range(hq):
+            g = h // (hq // hk)
+            q, key, v = (qkv[rows, c * dh:(c + 1) * dh] for c in (h, hq + g, hq + hk + g))
+            if n == 0:
+                continue
+            sc = np.where(seen, scale * (q @ key.T), -np.inf)
+            e = np.exp(sc - sc.max(axis=1, keepdims=True))
+            pr = e / e.sum(axis=1, keepdims=True)
+            out[rows, h * dh:(h + 1) * dh] = pr @ v
+            saved.append((rows, h, g, q, key, v, pr))
+    return out, (saved, scale)
+
+
+def attention_window_bwd(do, saved, op, b):
+    """As attention_bwd, per sample and query head; dK and dV add over the query heads that share them."""
+    s, hq, hk, dh = op["seq_len"], op["heads"], op["kv_heads"], op["head_dim"]
+    dx = np.zeros((b * s, (hq + 2 * hk) * dh))
+    saved, scale = saved
+    for rows, h, g, q, key, v, pr in saved:
+        d = do[rows, h * dh:(h + 1) * dh]
+        dp = d @ v.T
+        ds = pr * (dp - (dp * pr).sum(axis=1, keepdims=True))
+        dx[rows, h * dh:(h + 1) * dh] = scale * (ds @ key)
+        dx[rows, (hq + g) * dh:(hq + g + 1) * dh] += scale * (ds.T @ q)
+        dx[rows, (hq + hk + g) * dh:(hq + hk + g + 1) * dh] += pr.T @ d
+    return [dx]
+
+
 def meanpool_fwd(x, op, b):
     """Mean over the sequence positions of each sample: [b*S, d] -> [b, d]."""
     s = op["seq_len"]
@@ -405,6 +493,10 @@ class OracleStage:
                 val[i], st.saved[i] = layernorm_fwd(src[0], self.params[i], op)
             elif k == "attention":
                 val[i], st.saved[i] = attention_fwd(src[0], op, self.b)
+            elif k == "rotary":
+                val[i], st.saved[i] = rotary_fwd(src[0], src[1], op)
+            elif k == "attention_window":
+                val[i], st.saved[i] = attention_window_fwd(src[0], src[1] if len(src) == 2 else None, op, self.b)
             elif k == "add":
                 val[i] = src[0] + src[1]
             elif k == "meanpool":
@@ -458,6 +550,10 @@ class OracleStage:
                 dxs = layernorm_bwd(dy, st.saved[i], self.params[i], self.grads[i], op)
             elif k == "attention":
                 dxs = attention_bwd(dy, st.saved[i], op, self.b)
+            elif k == "rotary":
+                dxs = rotary_bwd(dy, st.saved[i], op)
+            elif k == "attention_window":
+                dxs = attention_window_bwd(dy, st.saved[i], op, self.b)
             elif k == "add":
                 dxs = [dy, dy]
             elif k == "meanpool":

@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 
 import numpy as np
 
@@ -24,7 +25,9 @@ STATUS_NAMES = ["GPP_OK", "GPP_ERR_INVALID_ARG", "GPP_ERR_BAD_GRAPH", "GPP_ERR_S
 DTYPES = {"f32": 0, "bf16": 1, "i32": 2}
 KINDS = {"input": 0, "linear": 1, "layernorm": 2, "attention": 3, "add": 4, "meanpool": 5, "concat": 6,
          "embedding_bag_sum": 7, "dot_interact": 8, "loss_mse": 9, "loss_ce": 10, "loss_bce": 11,
-         "embedding_bag_concat": 12}
+         "embedding_bag_concat": 12, "rotary": 13, "attention_window": 14}
+PAIRINGS = {"halves": 0, "neighbours": 1}
+LADDERS = {"shared": 0, "per_axis": 1}
 ACTS = {"none": 0, "relu": 1, "gelu": 2}
 FLAG_FORCE_GENERIC_GEMM = 1
 FLAG_SPLIT_K = 2
@@ -201,6 +204,14 @@ def build_desc(ops, micro_batch, slots=1, flags=0, param_ptrs=None, grad_ptrs=No
         for k in range(2):
             d.param[k] = (param_ptrs or {}).get(i, [None, None])[k]
             d.grad[k] = (grad_ptrs or {}).get(i, [None, None])[k]
+        # (these operators' own names for fields of the structure, see the unions of gpp_op_desc_t)
+        if op["kind"] == "rotary":
+            d.in_features, d.eps = op["head_dim"], op["base"]
+            d.act, d.has_bias = PAIRINGS[op.get("pairing", "halves")], LADDERS[op.get("ladder", "shared")]
+            d.num_rows = int.from_bytes(struct.pack("<4h", *(list(op["axis_pairs"]) + [0] * 4)[:4]), "little", signed=True)
+        elif op["kind"] == "attention_window":
+            d.in_features, d.rows_extra, d.eps = op["head_dim"], op["kv_heads"], op.get("scale", 0.0)
+            d.num_rows, d.bag_size, d.has_bias = op.get("window", 0), op.get("sinks", 0), 1 if op.get("causal", False) else 0
     sd = StageDesc(n, C.cast(arr, C.POINTER(OpDesc)), int(micro_batch), int(slots), int(flags))
     return sd, keep
 

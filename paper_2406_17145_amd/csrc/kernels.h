@@ -111,6 +111,46 @@ struct AttnProb {
   int32_t blk_begin;
 };
 
+// ---- rotary positions --------------------------------------------------------
+// one pair of columns: radians / (2 pi) per position, and the axis whose position it takes
+struct RotaryPair {
+  double turns;
+  int32_t axis, pad;
+};
+struct RotaryProb {
+  const GPP_G void *x;       // fwd: the rows; bwd: the gradient of the output
+  GPP_G void *y;             // fwd: output; bwd: gradient of the rows.  y == x: in place, columns that do not turn are not touched
+  const GPP_G int32_t *pos;  // [rows, axes]
+  GPP_G int32_t *pos_keep;   // fwd, or null: the positions are copied here for the backward pass
+  const GPP_G RotaryPair *table;   // [pairs]
+  int64_t ld_x, ld_y;
+  int32_t rows, cols, heads, dh, pairs, axes, dtype;
+  int32_t neighbours, backward, in_place;
+  int32_t ext_x, ext_y, ext_pos;   // >= 0: the pointer is this entry of the per-call pointer block (a null ext_y: not wanted)
+  int32_t rows_per_block, blk_begin;
+};
+
+// ---- attention inside a window -----------------------------------------------
+struct WindowProb {
+  const GPP_G void *qkv;   // [b*S, (heads + 2 kv_heads) dh]
+  GPP_G void *out;         // fwd: O [b*S, heads dh] or null; bwd: dqkv
+  GPP_G void *o;           // bwd: O (forward output)
+  const GPP_G void *dout;  // bwd: dO
+  GPP_G float *lse;        // [b*heads, S] log2 of the sum of 2^(scores in base 2); bwd reads it
+  GPP_G float *delta;      // bwd: [b*heads, S] rowsum(dO * O), written with dQ
+  const GPP_G int32_t *lengths;   // [b], or null with ext_len < 0: all S
+  GPP_G int32_t *lengths_keep;    // fwd, or null: the lengths are copied here for the backward pass
+  int64_t ld_qkv, ld_out, ld_o, ld_dout;
+  int64_t window, sinks;   // window 0: S (no limit)
+  int32_t batch, heads, kv_heads, seq, dh, causal;
+  float scale;
+  int32_t dtype, out_dtype, grad_dtype;   // qkv; O and dO; dqkv
+  // >= 0: entry of the per-call pointer block.  ext_out: fwd, O is written there too (entry may be null); bwd, dqkv goes there
+  int32_t ext_qkv, ext_out, ext_dout, ext_len;
+  int64_t ld_ext;          // fwd: row stride of the tensor behind ext_out
+  int32_t blk_begin;
+};
+
 // ---- mean-pool over the sequence -------------------------------------------
 struct PoolProb {
   const GPP_G void *src;
@@ -205,7 +245,7 @@ struct ExtPtrs {
 
 // per-stage device flags
 struct StageFlags {
-  int32_t index_error;    // an embedding index, a bag offset or a class label was out of range
+  int32_t index_error;    // an embedding index, a bag offset, a class label or a length was out of range
 };
 
 // ---- launch entry points (defined next to the kernels) -------------------------
@@ -308,6 +348,18 @@ int ln_rows_per_block();
 int ln_param_blocks(int d);
 
 int attn_blocks(int batch, int heads, int seq);
+
+// vec: elements that a lane moves at once (as rotary_vec names them)
+void launch_rotary(const RotaryProb *probs, int n, int total_blocks, int dtype, int vec, const ExtPtrs &ext, hipStream_t s);
+int rotary_vec(const RotaryProb &p);
+int rotary_rows_per_block(int64_t launch_rows, int pairs);
+int rotary_max_pairs();
+
+void launch_window_fwd(const WindowProb *probs, int n, int total_blocks, const ExtPtrs &ext, StageFlags *flags, hipStream_t s);
+void launch_window_dq(const WindowProb *probs, int n, int total_blocks, const ExtPtrs &ext, hipStream_t s);
+void launch_window_dkv(const WindowProb *probs, int n, int total_blocks, const ExtPtrs &ext, hipStream_t s);
+int window_max_head_dim();
+int window_blocks(int64_t batch, int heads, int seq);
 
 void launch_pool(const PoolProb *probs, int n, int total_blocks, hipStream_t s);
 int pool_blocks(const PoolProb &p);

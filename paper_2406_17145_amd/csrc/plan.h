@@ -29,9 +29,11 @@ enum Kern : int32_t {
   K_ELT, K_GEMM_GENERIC, K_GEMM_MFMA, K_COLSUM, K_LN_FWD, K_LN_BWD, K_LN_BWD_PARAMS, K_ATTN_FWD, K_ATTN_DQ,
   K_ATTN_DKV, K_POOL, K_EMB_FWD, K_EMB_BWD, K_INTERACT_FWD, K_INTERACT_BWD, K_LOSS_FWD, K_LOSS_BWD, K_LOSS_SUM,
   K_GEMM_SKINNY, K_GEMM_BWD_MERGED, K_LOSS_FWD_SMALL, K_GEMM_BIG, K_GEMM_DW_KSPLIT, K_GEMM_DW_GROUP, K_FORK, K_JOIN,
-  K_HEAD_LOSS, K_GEMM_SPLIT, K_GEMM_RING
+  K_HEAD_LOSS, K_GEMM_SPLIT, K_GEMM_RING, K_ROTARY, K_WINDOW_FWD, K_WINDOW_DQ, K_WINDOW_DKV
 };
-enum ExtKind : int32_t { EXT_NONE = 0, EXT_INPUTS, EXT_OUTPUTS, EXT_GRAD_OUTPUTS, EXT_GRAD_INPUTS };
+// EXT_BOTH: what the call reads (inputs, or output gradients) in the first half of the pointer block, what it writes in the second
+enum ExtKind : int32_t { EXT_NONE = 0, EXT_INPUTS, EXT_OUTPUTS, EXT_GRAD_OUTPUTS, EXT_GRAD_INPUTS, EXT_BOTH };
+constexpr int EXT_HALF = 32;
 
 struct Step {
   int32_t kern;
@@ -62,6 +64,11 @@ struct Node {
   int loss_index = -1;
   int emb_passes = 0, emb_sort_blocks = 0;
   bool grad_direct = false;  // input: its gradient is written straight into the caller's buffer by the producing GEMM
+  // Sequence operators (ROTARY, ATTENTION_WINDOW) work on the caller's tensors themselves where nothing else needs a copy:
+  bool read_direct = false;  // input: no copy in front of the forward pass (integers: the first of its readers keeps one for the backward pass)
+  bool out_direct = false;   // output: written into the caller's buffer, its gradient read from the caller's
+  bool gin_direct = false;   // input: its only consumer writes the gradient into the caller's buffer
+  bool in_place = false;     // ROTARY: turns its producer's value, and the gradient of that, where they lie
 };
 
 struct Plan {

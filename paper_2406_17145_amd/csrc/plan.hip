@@ -2,6 +2,7 @@
 #include "plan.h"
 
 #include <algorithm>
+#include <cmath>
 #include <cstring>
 #include <functional>
 
@@ -45,7 +46,7 @@ gpp_status_t Plan::analyse(const gpp_stage_desc_t *desc) {
   for (int i = 0; i < n; ++i) {
     Node &nd = nodes[i];
     nd.d = desc->ops[i];
-    if (nd.d.kind < GPP_OP_INPUT || nd.d.kind > GPP_OP_EMBEDDING_BAG_CONCAT) FAIL(GPP_ERR_INVALID_ARG, "unknown operator kind");
+    if (nd.d.kind < GPP_OP_INPUT || nd.d.kind > GPP_OP_ATTENTION_WINDOW) FAIL(GPP_ERR_INVALID_ARG, "unknown operator kind");
     if (nd.d.n_in < 0 || nd.d.n_in > 4096 || (nd.d.n_in > 0 && !nd.d.in)) FAIL(GPP_ERR_INVALID_ARG, "bad producer list");
     for (int k = 0; k < nd.d.n_in; ++k) {
       int p = nd.d.in[k];
@@ -66,7 +67,8 @@ gpp_status_t Plan::analyse(const gpp_stage_desc_t *desc) {
       case GPP_OP_LINEAR: case GPP_OP_LAYERNORM: case GPP_OP_ATTENTION: case GPP_OP_MEANPOOL_SEQ:
       case GPP_OP_DOT_INTERACT: want = 1; break;
       case GPP_OP_ADD: case GPP_OP_EMBEDDING_BAG_SUM: case GPP_OP_EMBEDDING_BAG_CONCAT: case GPP_OP_LOSS_MSE: case GPP_OP_LOSS_CE:
-      case GPP_OP_LOSS_BCE_LOGITS: want = 2; break;
+      case GPP_OP_LOSS_BCE_LOGITS: case GPP_OP_ROTARY: want = 2; break;
+      case GPP_OP_ATTENTION_WINDOW: want = nd.in.size() == 2 ? 2 : 1; break;      // (lengths are optional)
       default: break;
     }
     if (want >= 0 && (int)nd.in.size() != want) FAIL(GPP_ERR_BAD_GRAPH, "operator has the wrong number of producers");
@@ -132,6 +134,49 @@ gpp_status_t Plan::analyse(const gpp_stage_desc_t *desc) {
         if (d.out_features / d.heads > 128) FAIL(GPP_ERR_UNSUPPORTED, "attention: head dimension above 128");
         if (d.seq_len > attn_max_seq()) FAIL(GPP_ERR_UNSUPPORTED, "attention: sequence too long for this build");
         if (!is_float(d.dtype) || !is_float(in(0).d.dtype)) FAIL(GPP_ERR_UNSUPPORTED, "attention: float dtypes only");
+        break;
+      case GPP_OP_ROTARY: {
+        nd.rows = in(0).rows;
+        if (in(0).feat != d.out_features) FAIL(GPP_ERR_SHAPE, "rotary: feature count differs from the producer's");
+        if (!is_float(d.dtype) || d.dtype != in(0).d.dtype) FAIL(GPP_ERR_UNSUPPORTED, "rotary: a float output of the producer's dtype only");
+        if (d.heads <= 0 || d.head_dim <= 0 || d.head_dim > d.out_features || (int64_t)d.heads * d.head_dim > d.out_features)
+          FAIL(GPP_ERR_SHAPE, "rotary: heads * head_dim columns must lie inside the features");
+        if (d.out_features > (1 << 24)) FAIL(GPP_ERR_UNSUPPORTED, "rotary: more than 2^24 features");
+        int64_t axes = 0, pairs = 0;
+        for (int a = 0; a < 4; ++a) {
+          if (d.axis_pairs[a] < 0 || (d.axis_pairs[a] > 0 && axes < a)) FAIL(GPP_ERR_INVALID_ARG, "rotary: axis_pairs must be positive, axes that are not there last");
+          axes += d.axis_pairs[a] > 0;
+          pairs += d.axis_pairs[a];
+        }
+        if (axes == 0) FAIL(GPP_ERR_INVALID_ARG, "rotary: no axis");
+        if (2 * pairs > d.head_dim) FAIL(GPP_ERR_SHAPE, "rotary: more pairs than a head has columns for");
+        if (pairs > rotary_max_pairs()) FAIL(GPP_ERR_UNSUPPORTED, "rotary: too many pairs for this build");
+        if (!(d.base > 0) || !std::isfinite(d.base)) FAIL(GPP_ERR_INVALID_ARG, "rotary: base must be positive");
+        if (d.pairing != GPP_PAIR_HALVES && d.pairing != GPP_PAIR_NEIGHBOURS) FAIL(GPP_ERR_INVALID_ARG, "rotary: bad pairing");
+        if (d.ladder != GPP_LADDER_SHARED && d.ladder != GPP_LADDER_PER_AXIS) FAIL(GPP_ERR_INVALID_ARG, "rotary: bad ladder");
+        if (in(1).d.kind != GPP_OP_INPUT || in(1).d.dtype != GPP_I32) FAIL(GPP_ERR_BAD_GRAPH, "rotary: positions must be an i32 input");
+        if (in(1).rows != nd.rows || in(1).feat != axes) FAIL(GPP_ERR_SHAPE, "rotary: positions must be [rows, axes]");
+        break;
+      }
+      case GPP_OP_ATTENTION_WINDOW:
+        nd.rows = in(0).rows;
+        if (d.heads <= 0 || d.kv_heads <= 0 || d.heads % d.kv_heads) FAIL(GPP_ERR_SHAPE, "windowed attention: kv_heads must divide heads");
+        if (d.head_dim <= 0 || d.out_features % d.heads || d.out_features / d.heads != d.head_dim)
+          FAIL(GPP_ERR_SHAPE, "windowed attention: out_features must be heads * head_dim");
+        if (in(0).feat != d.out_features + 2 * (int64_t)d.kv_heads * d.head_dim)
+          FAIL(GPP_ERR_SHAPE, "windowed attention: producer must have (heads + 2*kv_heads)*head_dim columns (Q|K|V)");
+        if (d.seq_len <= 0 || nd.rows != micro_batch * d.seq_len) FAIL(GPP_ERR_SHAPE, "windowed attention: rows must equal micro_batch*seq_len");
+        if (d.head_dim > window_max_head_dim()) FAIL(GPP_ERR_UNSUPPORTED, "windowed attention: head dimension above 256");
+        if (d.seq_len > (1 << 30)) FAIL(GPP_ERR_UNSUPPORTED, "windowed attention: sequence too long for this build");
+        if (nd.rows * (int64_t)d.heads > (1 << 25)) FAIL(GPP_ERR_UNSUPPORTED, "windowed attention: too many rows and heads");
+        if (d.window < 0 || d.sinks < 0) FAIL(GPP_ERR_INVALID_ARG, "windowed attention: window and sinks must not be negative");
+        if (d.causal != 0 && d.causal != 1) FAIL(GPP_ERR_INVALID_ARG, "windowed attention: causal is 0 or 1");
+        if (!(d.scale >= 0) || !std::isfinite((float)d.scale)) FAIL(GPP_ERR_INVALID_ARG, "windowed attention: scale must be positive (0: 1/sqrt(head_dim))");
+        if (!is_float(d.dtype) || !is_float(in(0).d.dtype)) FAIL(GPP_ERR_UNSUPPORTED, "windowed attention: float dtypes only");
+        if (nd.in.size() == 2) {
+          if (in(1).d.kind != GPP_OP_INPUT || in(1).d.dtype != GPP_I32) FAIL(GPP_ERR_BAD_GRAPH, "windowed attention: lengths must be an i32 input");
+          if (in(1).rows != micro_batch || in(1).feat != 1) FAIL(GPP_ERR_SHAPE, "windowed attention: lengths must be [micro_batch, 1]");
+        }
         break;
       case GPP_OP_ADD:
         nd.rows = in(0).rows;
@@ -229,6 +274,28 @@ gpp_status_t Plan::analyse(const gpp_stage_desc_t *desc) {
     nd.gdtype = (k == GPP_OP_LINEAR) ? nd.d.param_dtype : nd.d.dtype;
   }
 
+  // ---- sequence operators on the caller's tensors ------------------------
+  // (an input that other operators read too is copied for them anyway; an attention whose input wants its gradient reads Q, K
+  // and V again in the backward pass, when the caller's tensor may be gone.  A rotary's backward pass takes its positions only)
+  auto sequence_op = [](const Node &x) { return x.d.kind == GPP_OP_ROTARY || x.d.kind == GPP_OP_ATTENTION_WINDOW; };
+  for (int i = 0; i < n; ++i) {
+    Node &nd = nodes[i];
+    if (nd.d.kind == GPP_OP_INPUT && nd.input_index < EXT_HALF) {
+      nd.read_direct = true;
+      for (int u : nd.users) {
+        const Node &c = nodes[u];
+        nd.read_direct = nd.read_direct && sequence_op(c) && !(c.d.kind == GPP_OP_ATTENTION_WINDOW && c.in[0] == i && c.wants_grad);
+      }
+      nd.gin_direct = nd.wants_grad && nd.users.size() == 1 && sequence_op(nodes[nd.users[0]]);
+    }
+    nd.out_direct = sequence_op(nd) && nd.is_output && nd.output_index < EXT_HALF;
+    // a layer that keeps nothing of its output (no activation, no addend) and hands it to a rotary only
+    if (nd.d.kind == GPP_OP_ROTARY && !nd.is_output) {
+      const Node &x = nodes[nd.in[0]];
+      nd.in_place = x.d.kind == GPP_OP_LINEAR && x.d.act == GPP_ACT_NONE && x.users.size() == 1 && x.gdtype == nd.gdtype;
+    }
+  }
+
   // ---- fusion / aliasing decisions -------------------------------------
   for (int i = 0; i < n; ++i) {
     Node &nd = nodes[i];
@@ -262,7 +329,7 @@ gpp_status_t Plan::analyse(const gpp_stage_desc_t *desc) {
       // slice does not start on 16 bytes gets a copy of its gradient: on the slice itself its two GEMMs would not run
       // on the matrix cores -- five [951 x 2036 x 2036] layers: 690 us each for both, the copy 30; nor do they with a copy
       // under flag bit 0)
-      const bool aligned = m.d.kind != GPP_OP_LINEAR || c.gdtype != DT_BF16 || col % 8 == 0 || (flags & 1);
+      const bool aligned = !(m.d.kind == GPP_OP_LINEAR || m.in_place) || c.gdtype != DT_BF16 || col % 8 == 0 || (flags & 1);
       if (sole && m.gdtype == c.gdtype && m.wants_grad && m.d.kind != GPP_OP_EMBEDDING_BAG_CONCAT) {
         if (aligned || no_copies) {
           m.gout_parent = i;
@@ -275,10 +342,11 @@ gpp_status_t Plan::analyse(const gpp_stage_desc_t *desc) {
     }
   }
   // (what multiplies a gradient by a derivative in place needs it to itself: a Linear with an activation, and a merge that
-  // such a Linear has its gradient in, directly or inside merges of merges; an ADD in between holds none, by this rule)
+  // such a Linear has its gradient in, directly or inside merges of merges; an ADD in between holds none, by this rule; so does a
+  // rotary that turns a gradient in place)
   auto activated = [](const Node &x) { return x.d.kind == GPP_OP_LINEAR && x.d.act != GPP_ACT_NONE; };
   std::function<bool(int)> multiplied = [&](int p) {
-    if (activated(nodes[p])) return true;
+    if (activated(nodes[p]) || nodes[p].in_place) return true;
     if (nodes[p].d.kind == GPP_OP_CONCAT)
       for (int q : nodes[p].in)
         if (nodes[q].gout_parent == p && multiplied(q)) return true;
@@ -298,6 +366,15 @@ gpp_status_t Plan::analyse(const gpp_stage_desc_t *desc) {
     }
   }
 
+  for (int i = 0; i < n; ++i)
+    if (nodes[i].in_place) {
+      Node &x = nodes[nodes[i].in[0]];
+      x.val_parent = i;
+      x.val_col = 0;
+      x.gout_parent = i;
+      x.gout_col = 0;
+    }
+
   // ---- buffers ----------------------------------------------------------
   int64_t slot_top = 0, shared_top = 0;
   auto alloc = [&](int32_t space, int64_t rows, int64_t cols, int32_t dt) {
@@ -315,6 +392,8 @@ gpp_status_t Plan::analyse(const gpp_stage_desc_t *desc) {
     Node &nd = nodes[i];
     if (nd.val.valid() || nd.is_loss) return;
     if (nd.d.kind == GPP_OP_LINEAR && nd.fused_add >= 0) return;  // lives in the ADD's buffer
+    if (nd.read_direct && nd.d.dtype != DT_I32) return;           // (and what the backward pass does not need of an output:)
+    if (nd.out_direct && !(nd.d.kind == GPP_OP_ATTENTION_WINDOW && nd.wants_grad)) return;
     if (nd.val_parent >= 0) {
       alloc_val(nd.val_parent);
       const Node &c = nodes[nd.val_parent];
@@ -328,7 +407,7 @@ gpp_status_t Plan::analyse(const gpp_stage_desc_t *desc) {
   for (int i = 0; i < n; ++i) alloc_val(i);
   std::function<void(int)> alloc_gout = [&](int i) {
     Node &nd = nodes[i];
-    if (nd.gout.valid() || nd.is_loss || !nd.wants_grad) return;
+    if (nd.gout.valid() || nd.is_loss || !nd.wants_grad || nd.out_direct || nd.gin_direct) return;
     if (nd.gout_parent >= 0) {
       alloc_gout(nd.gout_parent);
       const Node &c = nodes[nd.gout_parent];
@@ -384,6 +463,10 @@ gpp_status_t Plan::analyse(const gpp_stage_desc_t *desc) {
       }
     }
     if (d.kind == GPP_OP_ATTENTION) {
+      nd.stat0 = alloc(SP_SLOT, 1, micro_batch * d.heads * d.seq_len, DT_F32);    // log-sum-exp
+      nd.stat1 = alloc(SP_SHARED, 1, micro_batch * d.heads * d.seq_len, DT_F32);  // rowsum(dO*O)
+    }
+    if (d.kind == GPP_OP_ATTENTION_WINDOW && nd.wants_grad) {
       nd.stat0 = alloc(SP_SLOT, 1, micro_batch * d.heads * d.seq_len, DT_F32);    // log-sum-exp
       nd.stat1 = alloc(SP_SHARED, 1, micro_batch * d.heads * d.seq_len, DT_F32);  // rowsum(dO*O)
     }
@@ -494,6 +577,8 @@ struct Emitter {
     if (!recs.empty()) memcpy(pl.blob.data() + off, recs.data(), recs.size() * sizeof(T));
     return off;
   }
+  // where a table of this slot lies on the device
+  const char *table_ptr(int64_t off) const { return ws + pl.off_tables + (int64_t)slot * pl.table_bytes + off; }
   Step &add_step(int kern, int64_t table_off, int n, int blocks) {
     Step s;
     memset(&s, 0, sizeof(s));
@@ -597,6 +682,81 @@ struct Emitter {
     s.a2 = ps | (vec ? 256 : 0) | (odt << 9) | (md << 11);   // passes (8 bits), vector path, gradient dtype (2 bits), largest dimension
     s.launches = emb_bwd_num_launches(ps, vec ? 1 : 0);
     s.lane = lane;
+  }
+
+  // ---- sequence operators ------------------------------------------------
+  // of the readers of an integer input that the caller's tensor is read from: the one that keeps a copy for the backward pass
+  bool keeps(const Node &input, int reader) const {
+    for (int u : input.users)
+      if (pl.nodes[u].wants_grad) return u == reader;
+    return false;
+  }
+  RotaryProb rotary_record(const Node &nd, bool backward) {
+    const gpp_op_desc_t &d = nd.d;
+    RotaryProb r;
+    memset(&r, 0, sizeof(r));
+    std::vector<RotaryPair> table;
+    int total = 0;
+    for (int a = 0; a < 4; ++a) total += d.axis_pairs[a];
+    for (int a = 0; a < 4; ++a)
+      for (int j = 0; j < d.axis_pairs[a]; ++j) {
+        const double e = d.ladder == GPP_LADDER_PER_AXIS ? (double)j / d.axis_pairs[a] : (double)table.size() / total;
+        table.push_back({std::pow(d.base, -e) / 6.283185307179586476925, a, 0});
+      }
+    r.table = (const RotaryPair *)table_ptr(push_table(table));
+    r.rows = (int32_t)nd.rows;
+    r.cols = (int32_t)nd.feat;
+    r.heads = d.heads;
+    r.dh = (int32_t)d.head_dim;
+    r.pairs = total;
+    r.axes = (int32_t)pl.nodes[nd.in[1]].feat;
+    r.dtype = d.dtype;
+    r.neighbours = d.pairing == GPP_PAIR_NEIGHBOURS;
+    r.backward = backward;
+    r.ext_x = r.ext_y = r.ext_pos = -1;
+    return r;
+  }
+  // one launch per storage type and width of a lane's piece
+  void emit_rotaries(std::vector<RotaryProb> &recs) {
+    int64_t rows = 0;
+    for (auto &r : recs) rows += r.rows;
+    for (int32_t dt : {DT_F32, DT_BF16})
+      for (int vec = 8; vec >= 1; vec >>= 1) {
+        std::vector<RotaryProb> now;
+        int blocks = 0;
+        for (auto &r : recs) {
+          if (r.dtype != dt || rotary_vec(r) != vec) continue;
+          r.rows_per_block = rotary_rows_per_block(rows, r.pairs);
+          r.blk_begin = blocks;
+          blocks += (r.rows + r.rows_per_block - 1) / r.rows_per_block;
+          now.push_back(r);
+        }
+        if (now.empty()) continue;
+        Step &s = add_step(K_ROTARY, push_table(now), (int)now.size(), blocks);
+        s.ext_kind = EXT_BOTH;
+        s.a0 = dt;
+        s.a1 = vec;
+      }
+    recs.clear();
+  }
+  WindowProb window_record(const Node &nd) {
+    const gpp_op_desc_t &d = nd.d;
+    WindowProb a;
+    memset(&a, 0, sizeof(a));
+    a.batch = (int32_t)pl.micro_batch;
+    a.heads = d.heads;
+    a.kv_heads = d.kv_heads;
+    a.seq = d.seq_len;
+    a.dh = (int32_t)d.head_dim;
+    a.causal = d.causal;
+    a.window = d.window;
+    a.sinks = d.sinks;
+    a.scale = d.scale > 0 ? (float)d.scale : (float)(1.0 / std::sqrt((double)d.head_dim));
+    a.dtype = pl.nodes[nd.in[0]].d.dtype;
+    a.out_dtype = d.dtype;
+    a.ext_qkv = a.ext_out = a.ext_dout = a.ext_len = -1;
+    if (nd.in.size() == 2) a.lengths = (const int32_t *)ptr(pl.nodes[nd.in[1]].val);
+    return a;
   }
 
   // ---- elementwise helper ------------------------------------------------
@@ -1100,6 +1260,7 @@ void Emitter::forward() {
         emit_elt(recs, EXT_INPUTS, base);
         base = (int)k;
       }
+      if (nd.read_direct) continue;
       Buf src;
       src.space = SP_ABS;
       src.ld = nd.feat;
@@ -1116,6 +1277,8 @@ void Emitter::forward() {
     std::vector<GemmProb> gemms;
     std::vector<LnProb> lns;
     std::vector<AttnProb> attns;
+    std::vector<RotaryProb> rotaries;
+    std::vector<WindowProb> windows;
     std::vector<EltProb> elts;
     std::vector<PoolProb> pools;
     std::vector<EmbProb> embs;
@@ -1198,6 +1361,59 @@ void Emitter::forward() {
           a.seq = d.seq_len;
           a.dh = (int32_t)(nd.feat / d.heads);
           attns.push_back(a);
+          break;
+        }
+        case GPP_OP_ROTARY: {
+          const Node &x = N[nd.in[0]], &q = N[nd.in[1]];
+          RotaryProb r = rotary_record(nd, false);
+          if (x.read_direct) {
+            r.ext_x = x.input_index;
+            r.ld_x = x.feat;
+          } else {
+            r.x = ptr(x.val);
+            r.ld_x = x.val.ld;
+          }
+          if (nd.out_direct) {
+            r.ext_y = EXT_HALF + nd.output_index;
+            r.ld_y = nd.feat;
+          } else {
+            r.y = ptr(nd.val);
+            r.ld_y = nd.val.ld;
+          }
+          r.in_place = nd.in_place;
+          r.pos = (const int32_t *)ptr(q.val);
+          if (q.read_direct) {
+            r.ext_pos = q.input_index;
+            if (keeps(q, i)) r.pos_keep = (int32_t *)ptr(q.val);
+          }
+          rotaries.push_back(r);
+          break;
+        }
+        case GPP_OP_ATTENTION_WINDOW: {
+          const Node &x = N[nd.in[0]];
+          WindowProb a = window_record(nd);
+          if (x.read_direct) {
+            a.ext_qkv = x.input_index;
+            a.ld_qkv = x.feat;
+          } else {
+            a.qkv = ptr(x.val);
+            a.ld_qkv = x.val.ld;
+          }
+          a.out = ptr(nd.val);
+          a.ld_out = nd.val.ld;
+          if (nd.out_direct) {
+            a.ext_out = EXT_HALF + nd.output_index;
+            a.ld_ext = nd.feat;
+          }
+          a.lse = (float *)ptr(nd.stat0);
+          if (nd.in.size() == 2) {
+            const Node &q = N[nd.in[1]];
+            if (q.read_direct) {
+              a.ext_len = q.input_index;
+              if (keeps(q, i)) a.lengths_keep = (int32_t *)ptr(q.val);
+            }
+          }
+          windows.push_back(a);
           break;
         }
         case GPP_OP_ADD: {
@@ -1389,6 +1605,15 @@ void Emitter::forward() {
       s.a0 = ms;
       s.a1 = mfma ? 1 : 0;
     }
+    emit_rotaries(rotaries);
+    if (!windows.empty()) {
+      int blocks = 0;
+      for (auto &a : windows) {
+        a.blk_begin = blocks;
+        blocks += window_blocks(a.batch, a.heads, a.seq);
+      }
+      add_step(K_WINDOW_FWD, push_table(windows), (int)windows.size(), blocks).ext_kind = EXT_BOTH;
+    }
     emit_elt(elts);
     if (!pools.empty()) {
       int blocks = 0;
@@ -1452,6 +1677,7 @@ void Emitter::forward() {
         emit_elt(recs, EXT_OUTPUTS, base);
         base = (int)k;
       }
+      if (nd.out_direct) continue;
       Buf dst;
       dst.space = SP_ABS;
       dst.ld = nd.feat;
@@ -1509,13 +1735,15 @@ void Emitter::backward() {
         base = (int)k;
       }
       if (!nd.wants_grad) continue;
-      Buf src;
-      src.space = SP_ABS;
-      src.ld = nd.feat;
-      src.dtype = nd.d.dtype;
-      EltProb e = elt(src, nd.gout, nd.rows, nd.feat);
-      e.ext_src = (int32_t)(k - base);
-      recs.push_back(e);
+      if (!nd.out_direct) {
+        Buf src;
+        src.space = SP_ABS;
+        src.ld = nd.feat;
+        src.dtype = nd.d.dtype;
+        EltProb e = elt(src, nd.gout, nd.rows, nd.feat);
+        e.ext_src = (int32_t)(k - base);
+        recs.push_back(e);
+      }
       gstate[pl.output_ops[k]] = G_WRITTEN;
       written_level[pl.output_ops[k]] = (int)pl.by_level.size();
     }
@@ -1610,6 +1838,8 @@ void Emitter::backward() {
       return turns[t];
     };
     std::vector<AttnProb> attns;
+    std::vector<RotaryProb> rotaries;
+    std::vector<WindowProb> windows;
     std::vector<PoolProb> pools;
     std::vector<EmbProb> embs;
     std::vector<InteractProb> inters;
@@ -1786,6 +2016,65 @@ void Emitter::backward() {
           attns.push_back(a);
           break;
         }
+        case GPP_OP_ROTARY: {
+          const Node &x = N[nd.in[0]];
+          if (!x.wants_grad) break;
+          RotaryProb r = rotary_record(nd, true);
+          r.pos = (const int32_t *)ptr(N[nd.in[1]].val);
+          if (nd.out_direct) {
+            r.ext_x = nd.output_index;
+            r.ld_x = nd.feat;
+          } else {
+            r.x = ptr(nd.gout);
+            r.ld_x = nd.gout.ld;
+          }
+          r.in_place = nd.in_place;
+          if (nd.in_place) {
+            r.y = ptr(nd.gout);
+            r.ld_y = nd.gout.ld;
+          } else if (x.gin_direct) {
+            r.ext_y = EXT_HALF + x.input_index;
+            r.ld_y = x.feat;
+            gstate[nd.in[0]] = G_WRITTEN;
+          } else {
+            const Target tg = acquire(nd.in[0], ADDS_NOT);
+            r.y = ptr(tg.dst);
+            r.ld_y = tg.dst.ld;
+          }
+          rotaries.push_back(r);
+          break;
+        }
+        case GPP_OP_ATTENTION_WINDOW: {
+          const Node &x = N[nd.in[0]];
+          if (!x.wants_grad) break;
+          WindowProb a = window_record(nd);
+          a.qkv = ptr(x.val);
+          a.ld_qkv = x.val.ld;
+          if (x.gin_direct) {
+            a.ext_out = EXT_HALF + x.input_index;
+            a.ld_out = x.feat;
+            a.grad_dtype = x.gdtype;
+            gstate[nd.in[0]] = G_WRITTEN;
+          } else {
+            const Target tg = acquire(nd.in[0], ADDS_NOT);
+            a.out = ptr(tg.dst);
+            a.ld_out = tg.dst.ld;
+            a.grad_dtype = tg.dst.dtype;
+          }
+          if (nd.out_direct) {
+            a.ext_dout = nd.output_index;
+            a.ld_dout = nd.feat;
+          } else {
+            a.dout = ptr(nd.gout);
+            a.ld_dout = nd.gout.ld;
+          }
+          a.o = ptr(nd.val);
+          a.ld_o = nd.val.ld;
+          a.lse = (float *)ptr(nd.stat0);
+          a.delta = (float *)ptr(nd.stat1);
+          windows.push_back(a);
+          break;
+        }
         case GPP_OP_ADD:
           pass_through(nd.in[0], nd.gout);
           pass_through(nd.in[1], nd.gout);
@@ -1918,6 +2207,21 @@ void Emitter::backward() {
       s2.a0 = ms;
       s2.a1 = mfma ? 1 : 0;
     }
+    if (!windows.empty()) {
+      int blocks = 0;
+      for (auto &a : windows) {
+        a.blk_begin = blocks;
+        blocks += window_blocks(a.batch, a.heads, a.seq);
+      }
+      add_step(K_WINDOW_DQ, push_table(windows), (int)windows.size(), blocks).ext_kind = EXT_BOTH;
+      blocks = 0;
+      for (auto &a : windows) {
+        a.blk_begin = blocks;
+        blocks += window_blocks(a.batch, a.kv_heads, a.seq);
+      }
+      add_step(K_WINDOW_DKV, push_table(windows), (int)windows.size(), blocks).ext_kind = EXT_BOTH;
+    }
+    emit_rotaries(rotaries);
     if (!pools.empty()) {
       int blocks = 0;
       for (auto &p : pools) {
@@ -1988,7 +2292,7 @@ void Emitter::backward() {
         emit_elt(recs, EXT_GRAD_INPUTS, base);
         base = (int)k;
       }
-      if (!nd.wants_grad || nd.grad_direct || state_of(pl.input_ops[k]) != G_WRITTEN) continue;
+      if (!nd.wants_grad || nd.grad_direct || nd.gin_direct || state_of(pl.input_ops[k]) != G_WRITTEN) continue;
       Buf dst;
       dst.space = SP_ABS;
       dst.ld = nd.feat;

@@ -104,9 +104,10 @@ static int step_tag(const Step &sp, bool backward) {
     case K_LN_FWD: return 9;
     case K_LN_BWD: return 10;
     case K_LN_BWD_PARAMS: return 11;
-    case K_ATTN_FWD: return 12;
-    case K_ATTN_DQ: return 13;
-    case K_ATTN_DKV: return 14;
+    case K_ROTARY: return backward ? 7 : 6;
+    case K_ATTN_FWD: case K_WINDOW_FWD: return 12;
+    case K_ATTN_DQ: case K_WINDOW_DQ: return 13;
+    case K_ATTN_DKV: case K_WINDOW_DKV: return 14;
     case K_POOL: return backward ? 16 : 15;
     case K_EMB_FWD: return 17;
     case K_EMB_BWD: return 18;
@@ -468,7 +469,13 @@ static gpp_status_t run_steps(gpp_stage *st, const std::vector<Step> &steps, int
     // per-call pointers the step's records refer to by index
     ExtPtrs ext;
     memset(&ext, 0, sizeof(ext));
-    if (sp.ext_kind != EXT_NONE) {
+    if (sp.ext_kind == EXT_BOTH) {
+      const int n_in = (int)pl.input_ops.size(), n_out = (int)pl.output_ops.size();
+      for (int k = 0; k < EXT_HALF; ++k) {
+        if (k < (is_bwd ? n_out : n_in)) ext.p[k] = ext_in ? (void *)ext_in[k] : nullptr;
+        if (k < (is_bwd ? n_in : n_out)) ext.p[EXT_HALF + k] = ext_out ? ext_out[k] : nullptr;
+      }
+    } else if (sp.ext_kind != EXT_NONE) {
       const bool in_side = sp.ext_kind == EXT_INPUTS || sp.ext_kind == EXT_GRAD_OUTPUTS;
       const int total = (sp.ext_kind == EXT_INPUTS || sp.ext_kind == EXT_GRAD_INPUTS) ? (int)pl.input_ops.size()
                                                                                      : (int)pl.output_ops.size();
@@ -531,6 +538,10 @@ static gpp_status_t run_steps(gpp_stage *st, const std::vector<Step> &steps, int
         if (sp.a1) launch_attn_bwd_dkv_mfma((const AttnProb *)tab, sp.n, sp.blocks, s);
         else launch_attn_bwd_dkv((const AttnProb *)tab, sp.n, sp.blocks, sp.a0, s);
         break;
+      case K_ROTARY: launch_rotary((const RotaryProb *)tab, sp.n, sp.blocks, sp.a0, sp.a1, ext, s); break;
+      case K_WINDOW_FWD: launch_window_fwd((const WindowProb *)tab, sp.n, sp.blocks, ext, flags, s); break;
+      case K_WINDOW_DQ: launch_window_dq((const WindowProb *)tab, sp.n, sp.blocks, ext, s); break;
+      case K_WINDOW_DKV: launch_window_dkv((const WindowProb *)tab, sp.n, sp.blocks, ext, s); break;
       case K_POOL: launch_pool((const PoolProb *)tab, sp.n, sp.blocks, s); break;
       case K_EMB_FWD: launch_emb_fwd((const EmbProb *)tab, sp.n, sp.blocks, sp.a0, sp.a1, flags, s); break;
       case K_EMB_BWD: {
@@ -989,7 +1000,7 @@ gpp_status_t gpp_stage_sync_status(gpp_stage_t *st, void *hip_stream) {
   if (he != hipSuccess) return fail(GPP_ERR_DEVICE, std::string("HIP: ") + hipGetErrorString(he));
   if (f.index_error) {
     hipMemset(st->ws + st->plan.off_flags, 0, sizeof(f));
-    return fail(GPP_ERR_INDEX, "an embedding index or offset was out of range");
+    return fail(GPP_ERR_INDEX, "an embedding index or offset, a class label or a length was out of range");
   }
   return GPP_OK;
 }

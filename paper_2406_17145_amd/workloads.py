@@ -17,6 +17,8 @@ Graph vocabulary (one dict per operator, `inputs` are producer op ids):
   linear     y = act(x W^T + b), W is [out_features, in_features]
   layernorm  over the feature dimension, affine (gamma, beta), eps
   attention  input [b*S, 3d] = (Q|K|V) column blocks, `heads` heads, softmax(QK^T/sqrt(dh))V
+  rotary     inputs (x, positions [rows, axes]); turns the first `heads` blocks of `head_dim` columns
+  attention_window  inputs (Q|K|V rows[, lengths]); `heads` and `kv_heads` of `head_dim`, window, sinks, causal
   add        elementwise sum of two producers
   meanpool   mean over the seq_len rows of each sample
   concat     feature-wise concatenation
@@ -199,17 +201,35 @@ def candle_uno(micro_batch=64, n_micro=8, seed=2, widths=(942, 3820, 2048, 1), h
 # config 3: multi-modal-transformer-shaped stage
 # --------------------------------------------------------------------------
 def mmt(micro_batch=4, n_micro=1, seed=3, n_branches=4, n_layers=2, d_model=1024, heads=16,
-        d_ff=4096, seq_len=512, d_head_out=1024, n_classes=1000, dtype=BF16):
+        d_ff=4096, seq_len=512, d_head_out=1024, n_classes=1000, dtype=BF16, kv_heads=None, axis_pairs=None,
+        window=0, sinks=0, causal=False, ragged=False):
+    """`axis_pairs`: branches whose tokens have positions (one per branch, e.g. a line of text, patches of an image,
+    patches of a video) and see a window around them, with `kv_heads` shared key / value heads and, where `ragged`,
+    samples of unequal lengths; None: plain attention over all tokens, without positions."""
     g = _Graph()
-    pooled = []
+    pooled, positions, lengths = [], [], []
+    dh = d_model // heads
     for br in range(n_branches):
         x = g.input(d_model, dtype, branch=br, seq_len=seq_len)
+        if axis_pairs:
+            positions.append(g.input(len(axis_pairs[br]), I32, branch=br, seq_len=seq_len, role="positions"))
+            if ragged:
+                lengths.append(g.input(1, I32, branch=br, role="lengths"))
         for _ in range(n_layers):
             a = g.add("layernorm", (x,), out_features=d_model, eps=1e-5, dtype=dtype, branch=br,
                       seq_len=seq_len)
-            qkv = g.linear(a, d_model, 3 * d_model, "none", dtype, branch=br)
-            o = g.add("attention", (qkv,), out_features=d_model, heads=heads, seq_len=seq_len,
-                      dtype=dtype, branch=br)
+            if axis_pairs:
+                kv = kv_heads or heads
+                qkv = g.linear(a, d_model, (heads + 2 * kv) * dh, "none", dtype, branch=br)
+                qkv = g.add("rotary", (qkv, positions[br]), out_features=(heads + 2 * kv) * dh, heads=heads + kv, head_dim=dh,
+                            axis_pairs=list(axis_pairs[br]), base=10000.0, seq_len=seq_len, dtype=dtype, branch=br)
+                o = g.add("attention_window", (qkv, lengths[br]) if ragged else (qkv,), out_features=d_model, heads=heads,
+                          kv_heads=kv, head_dim=dh, window=window, sinks=sinks, causal=causal, seq_len=seq_len, dtype=dtype,
+                          branch=br)
+            else:
+                qkv = g.linear(a, d_model, 3 * d_model, "none", dtype, branch=br)
+                o = g.add("attention", (qkv,), out_features=d_model, heads=heads, seq_len=seq_len,
+                          dtype=dtype, branch=br)
             p = g.linear(o, d_model, d_model, "none", dtype, branch=br)
             h = g.add("add", (x, p), out_features=d_model, dtype=dtype, branch=br)
             c = g.add("layernorm", (h,), out_features=d_model, eps=1e-5, dtype=dtype, branch=br,
@@ -227,6 +247,10 @@ def mmt(micro_batch=4, n_micro=1, seed=3, n_branches=4, n_layers=2, d_model=1024
     rng = np.random.Generator(np.random.PCG64(seed))
     params = _draw_params(g.ops, rng)
     samplers = {lab: lambda r, s: r.integers(0, n_classes, s)}
+    for p in positions:
+        samplers[p] = lambda r, s: r.integers(0, 1000, s)
+    for p in lengths:
+        samplers[p] = lambda r, s: r.integers(0, seq_len + 1, s)
     batches = _draw_batches(g.ops, micro_batch, n_micro, rng, samplers)
     return Workload("mmt", g.ops, micro_batch, n_micro, params, batches,
                     2e-2 if dtype == BF16 else 1e-4)
