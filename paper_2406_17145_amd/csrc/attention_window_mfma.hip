@@ -1,0 +1,919 @@
+// Windowed attention on the matrix cores, head dimensions up to 128 in bf16 or fp32 (see attention_window.hip for the mathematics).
+//
+// A workgroup of four waves owns 128 rows (queries: forward, dQ; keys: dK and dV), 32 per wave, whose operands stay in registers; the
+// other side streams through LDS in tiles, copied from memory straight into LDS, two buffers: tile t + 1 arrives while tile t
+// is multiplied.  Only tiles that hold a visible pair are streamed, only waves that have one in a tile multiply it, and only
+// where the window's edge, the diagonal, the last first token or the end of the sample crosses a wave's 32 rows are
+// elements masked.  Rows behind a sample's length read as zero.
+//
+// v_mfma_f32_32x32 leaves lane l with column l % 32 of the result and 16 of its rows.  Every score product is arranged so that what a
+// lane holds of it is, without any exchange between lanes, an operand of the next product: the 8 contraction slots that a lane
+// feeds into a step of 16 are accumulator registers 8c .. 8c + 7, score rows 16c + {0..3, 8..11} + 4 (l / 32), and the other operand
+// is read from LDS at those rows.
+//   forward      S^T = K Q^T              O^T  += V^T P^T
+//   backward dQ  S^T = K Q^T, dP^T = V dO^T,  dQ^T += K^T dS^T
+//   backward dKV S   = Q K^T, dP   = dO V^T,  dV += P^T dO,  dK += dS^T Q
+// P and dS enter the second products in the storage type, as operands of the matrix cores; all sums are fp32.  No atomics: dQ has
+// its own kernel, and sums over a long run of queries that are split over workgroups meet in a fixed order.
+#include <algorithm>
+
+#include "gemm_direct.h"
+#include "window_utils.h"
+
+namespace gpp {
+
+typedef __attribute__((ext_vector_type(8))) float f32x8;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+
+constexpr int WIN_ROWS = 128;     // rows that a workgroup owns
+
+// A tile row of DH elements takes RB bytes of LDS, half a bank line, a whole one or two, in chunks of 16 bytes; the 1 KB that a copy
+// instruction of a wave fills (RPG rows) is followed by 16 bytes of padding.  Chunk c of row r lies at position c ^ win_swizzle(r)
+// of its row.  Together they keep both reads out of each other's banks: along rows, 16 lanes read the same chunk of 16 consecutive
+// rows (the swizzle spreads the rows of a group over the quarters of a line, the padding moves group after group on by a
+// chunk); across rows, the transposing read takes 64 bytes of each of four consecutive rows (each row another quarter).  A swizzle
+// alone would do, but one that touches more bits of c costs every read of a row an address of its own.
+template <int RB>
+__device__ __forceinline__ int win_swizzle(int row) {
+  return RB == 128 ? (((row >> 1) & 1) << 2) | (((row >> 2) & 1) << 1) : (RB == 256 ? (row & 3) << 2 : (row & 1) << 3);
+}
+
+template <typename T, int DH>
+struct WinTile {
+  static constexpr int ES = sizeof(T), RB = DH * ES <= 128 ? 128 : (DH * ES <= 256 ? 256 : 512), CPR = RB / 16, EPC = 16 / ES;
+  static constexpr int KT = RB == 512 ? 32 : 64;     // rows of a streamed tile (fp32 rows of 512 bytes: two buffers of two tiles are 65 KB)
+  static constexpr int GROUP = 1040, RPG = 1024 / RB;
+  static constexpr int SUB = KT / 32, BYTES = KT / RPG * GROUP;
+  static constexpr int KS = DH / 16, DB = DH / 32;
+  static __host__ __device__ constexpr int at(int row) { return row / RPG * GROUP + row % RPG * RB; }
+};
+
+// ---- operands ---------------------------------------------------------------------------------------------
+template <typename T>
+struct WinFrag;
+template <>
+struct WinFrag<uint16_t> {
+  typedef bf16x8 type;
+  static __device__ __forceinline__ f32x16 mma(const bf16x8 &a, const bf16x8 &b, const f32x16 &c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+  }
+  static __device__ __forceinline__ bf16x8 pack(const f32x16 &v, int c) {
+    bf16x8 r;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) r[e] = (bf16_t)v[8 * c + e];
+    return r;
+  }
+  static __device__ __forceinline__ float get(const bf16x8 &a, int e) { return (float)a[e]; }
+};
+template <>
+struct WinFrag<float> {
+  typedef f32x8 type;
+  // (the order of a contraction does not matter: slot e of both lane halves is one step of two)
+  static __device__ __forceinline__ f32x16 mma(const f32x8 &a, const f32x8 &b, f32x16 c) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], b[e], c, 0, 0, 0);
+    return c;
+  }
+  static __device__ __forceinline__ f32x8 pack(const f32x16 &v, int c) {
+    f32x8 r;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) r[e] = v[8 * c + e];
+    return r;
+  }
+  static __device__ __forceinline__ float get(const f32x8 &a, int e) { return a[e]; }
+};
+
+// operand rows that a wave keeps: lane's row, columns 16 s + 8 (l / 32) .. of step s; columns beyond the head are zero
+template <typename T, int DH>
+struct WinRows {
+  typename WinFrag<T>::type f[DH / 16];
+};
+template <typename T, int DH>
+__device__ __forceinline__ WinRows<T, DH> win_rows(const GPP_G void *base, int64_t row, int64_t ld, int64_t col0, int dh) {
+  const int h = (threadIdx.x & 63) >> 5;
+  const GPP_G T *p = (const GPP_G T *)base + row * ld + col0;
+  constexpr int EPC = 16 / sizeof(T);
+  WinRows<T, DH> r;
+#pragma unroll
+  for (int s = 0; s < DH / 16; ++s) {
+    u32x4 part[8 / EPC];
+#pragma unroll
+    for (int k = 0; k < 8 / EPC; ++k) {
+      const int col = 16 * s + 8 * h + k * EPC;
+      part[k] = *(const GPP_G u32x4 *)(p + (col < dh ? col : 0));
+#pragma unroll
+      for (int e = 0; e < 4; ++e) part[k][e] = col < dh ? part[k][e] : 0u;
+    }
+    __builtin_memcpy(&r.f[s], part, sizeof(part));
+  }
+  return r;
+}
+// A lane's addresses inside a tile: of its row's chunks (read along rows) and of its column blocks (read across rows), as far as
+// the swizzle makes them differ; everything else about a read is a constant offset.
+template <typename T, int DH>
+struct WinLane {
+  typedef WinTile<T, DH> C;
+  static constexpr int NR = C::ES == 2 ? (C::RB == 128 ? C::KS : (C::KS + 1) / 2) : (C::RB == 512 ? 2 : C::KS);
+  uint32_t row[NR], col[C::DB];
+  // variant and constant offset of step s of a row
+  static __device__ __forceinline__ constexpr int variant(int s) { return C::ES == 2 ? (C::RB == 128 ? s : s >> 1) : (C::RB == 512 ? (s >> 1) & 1 : s); }
+  static __device__ __forceinline__ constexpr int offset(int s) {
+    return C::ES == 2 ? (C::RB == 128 ? 0 : (s & 1) * 32) : (C::RB == 512 ? (s >> 2) * 256 + (s & 1) * 64 : 0);
+  }
+};
+template <typename T, int DH>
+__device__ __forceinline__ WinLane<T, DH> win_lane() {
+  typedef WinTile<T, DH> C;
+  typedef WinLane<T, DH> L;
+  const int l = threadIdx.x & 63, row = l & 31;
+  L r;
+#pragma unroll
+  for (int s = C::KS - 1; s >= 0; --s)      // (of the steps that share a variant the first one's address, without its offset)
+    r.row[L::variant(s)] = C::at(row) + ((((16 * s + 8 * (l >> 5)) / C::EPC) ^ win_swizzle<C::RB>(row)) << 4) - L::offset(s);
+  const int blk = l >> 4, q = l & 15, cr = 4 * (blk >> 1) + (q >> 2);
+#pragma unroll
+  for (int d = 0; d < C::DB; ++d) {
+    const int col = 32 * d + 16 * (blk & 1) + 4 * (q & 3);
+    r.col[d] = C::ES == 2 ? C::at(cr) + (((col >> 3) ^ win_swizzle<C::RB>(cr)) << 4) + (col & 7) * 2 : 0;
+  }
+#pragma unroll
+  for (int k = 0; k < L::NR; ++k) asm("" : "+v"(r.row[k]));      // kept as they are: not formed again at every read
+  if constexpr (C::ES == 2) {
+#pragma unroll
+    for (int d = 0; d < C::DB; ++d) asm("" : "+v"(r.col[d]));
+  }
+  return r;
+}
+// lane takes row row0 + l % 32, columns 16 s + 8 (l / 32) .. (row0: a multiple of 32)
+template <typename T, int DH>
+__device__ __forceinline__ typename WinFrag<T>::type win_row_frag(const WinLane<T, DH> &lane, const unsigned char *tile, int row0, int s) {
+  typedef WinTile<T, DH> C;
+  typedef WinLane<T, DH> L;
+  const unsigned char *p = tile + lane.row[L::variant(s)] + (C::at(row0) + L::offset(s));
+  u32x4 part[8 / C::EPC];
+#pragma unroll
+  for (int k = 0; k < 8 / C::EPC; ++k) part[k] = *(const u32x4 *)(p + 16 * k);
+  typename WinFrag<T>::type r;
+  __builtin_memcpy(&r, part, sizeof(part));
+  return r;
+}
+// lane takes column 32 d + l % 32 of rows row0 + {0..3, 8..11} + 4 (l / 32) (row0: a multiple of 16)
+template <typename T, int DH>
+__device__ __forceinline__ typename WinFrag<T>::type win_col_frag(const WinLane<T, DH> &lane, const unsigned char *tile, int row0, int d) {
+  typedef WinTile<T, DH> C;
+  if constexpr (sizeof(T) == 2) {
+    typedef __attribute__((address_space(3))) s16x4 lds_v4;
+    const unsigned char *p = tile + lane.col[d] + C::at(row0);
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4 *)p), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4 *)(p + C::at(8)));
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+  } else {
+    const int l = threadIdx.x & 63, col = 32 * d + (l & 31);
+    f32x8 r;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int row = (e & 3) + 8 * (e >> 2) + 4 * (l >> 5);
+      r[e] = *(const float *)(tile + C::at(row0) + C::at(row) + (((col >> 2) ^ win_swizzle<C::RB>(row)) << 4) + (col & 3) * 4);
+    }
+    return r;
+  }
+}
+__device__ __forceinline__ f32x16 win_zero() {
+  f32x16 z;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) z[r] = 0.0f;
+  return z;
+}
+// row of a 32-row result that register r of this lane holds
+__device__ __forceinline__ int win_acc_row(int r) { return 8 * (r >> 2) + 4 * ((threadIdx.x & 63) >> 5) + (r & 3); }
+
+// maximum and sum of a lane and its partner 32 lanes on
+__device__ __forceinline__ float win_half_max(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float win_half_sum(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// ---- copies into LDS -----------------------------------------------------------------------------------------
+// where this lane's pieces of a tile lie behind the tile's first row: copy q of wave w of NW fills the KB w * N + q of the tile
+template <typename T, int DH, int NW>
+struct WinCopy {
+  static constexpr int N = WinTile<T, DH>::KT / WinTile<T, DH>::RPG / NW;
+  uint32_t off[N];
+};
+template <typename T, int DH, int NW>
+__device__ __forceinline__ WinCopy<T, DH, NW> win_copy_offsets(int wave, int64_t ld, int dh) {
+  typedef WinTile<T, DH> C;
+  const int l = threadIdx.x & 63;
+  WinCopy<T, DH, NW> r;
+#pragma unroll
+  for (int q = 0; q < r.N; ++q) {
+    const int row = (wave * r.N + q) * C::RPG + l / C::CPR, c = (l % C::CPR) ^ win_swizzle<C::RB>(row);
+    r.off[q] = c * C::EPC < dh ? (uint32_t)(row * ld * C::ES) + c * 16 : OOB_OFFSET;
+  }
+  return r;
+}
+__device__ __forceinline__ rsrc4 win_rsrc(const GPP_G void *base, uint32_t bytes) {
+  const uint64_t a = (uint64_t)base;
+  return (rsrc4){(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)a),
+                 (uint32_t)__builtin_amdgcn_readfirstlane((int)((uint32_t)(a >> 32) & 0xffffu)),
+                 (uint32_t)__builtin_amdgcn_readfirstlane((int)bytes), 0x00020000u};
+}
+template <typename T, int DH, int NW>
+__device__ __forceinline__ void win_copy(rsrc4 rs, const WinCopy<T, DH, NW> &o, uint32_t dst, int wave) {
+#pragma unroll
+  for (int q = 0; q < o.N; ++q) lds_copy16(rs, dst + (wave * o.N + q) * WinTile<T, DH>::GROUP, o.off[q]);
+}
+// 4 bytes per lane to consecutive LDS words (as lds_copy16)
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+__device__ __forceinline__ void lds_copy4(rsrc4 rs, uint32_t dst, uint32_t off) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(dst), "v"(off), "s"(rs) : "m0");
+}
+#pragma clang diagnostic pop
+// bytes of a tile's valid rows: rows [first, len) of it, at most KT, dh columns of the last
+__device__ __forceinline__ uint32_t win_tile_bytes(int rows, int64_t ld, int dh, int es) {
+  return rows <= 0 ? 0u : (uint32_t)(((int64_t)(rows - 1) * ld + dh) * es);
+}
+
+// neighbouring units for the workgroups of an XCD: consecutive workgroups go round the eight XCDs
+__device__ __forceinline__ int win_spread(int idx, int total) {
+  const int xcd = idx & 7, per = total >> 3, rem = total & 7;
+  return xcd * per + min(xcd, rem) + (idx >> 3);
+}
+
+// ---- which tiles of keys a block of queries streams -------------------------------------------------------------------
+struct WinRange {
+  int n, sinks, first;      // tiles: [0, sinks) and then [first, first + n - sinks)
+  __device__ __forceinline__ int tile(int t) const { return t < sinks ? t : first + t - sinks; }
+};
+template <int KT>
+__device__ __forceinline__ WinRange win_range(const WindowProb &p, int q0, int q1, int len) {
+  WinRange r = {0, 0, 0};
+  if (q0 >= len) return r;
+  const WindowKeys a = window_keys(p, q0, len), b = window_keys(p, q1, len);
+  r.first = a.first / KT;
+  r.sinks = min((b.sink_end + KT - 1) / KT, r.first);
+  r.n = r.sinks + (b.end - 1) / KT - r.first + 1;
+  return r;
+}
+// what of a tile of keys a wave's queries [q0, q1] see: nothing, all of it, or some
+enum { WIN_NONE, WIN_ALL, WIN_SOME };
+struct WinWave {
+  int first0, first1, end0, end1, sink0, sink1;      // of the first and the last query
+  bool active;
+  __device__ __forceinline__ int sees(int k0, int kt) const {
+    if (!active || !((k0 < end1 && k0 + kt > first0) || k0 < sink1)) return WIN_NONE;
+    return (k0 >= first1 && k0 + kt <= end0) || k0 + kt <= sink0 ? WIN_ALL : WIN_SOME;
+  }
+};
+__device__ __forceinline__ WinWave win_wave(const WindowProb &p, int q0, int len) {
+  WinWave w;
+  w.active = q0 < len;
+  const WindowKeys a = window_keys(p, min(q0, len - 1), len), b = window_keys(p, min(q0 + 31, len - 1), len);
+  w.first0 = a.first;
+  w.first1 = b.first;
+  w.end0 = a.end;
+  w.end1 = b.end;
+  w.sink0 = a.sink_end;
+  w.sink1 = b.sink_end;
+  return w;
+}
+
+// block of queries: key / value heads outermost, the query heads that share one innermost: workgroups that run together read the same
+// keys.  Where a causal block's work grows with its place, light and heavy blocks alternate, so that every XCD's share weighs the same
+struct WinBlock {
+  int b, h, r0;
+};
+__device__ __forceinline__ WinBlock win_query_block(const WindowProb &p, int blk) {
+  const int group = p.heads / p.kv_heads, nb = (p.seq + WIN_ROWS - 1) / WIN_ROWS;
+  const int hh = blk % group, rest = blk / group, k = rest % nb, bg = rest / nb;
+  WinBlock w;
+  w.b = bg / p.kv_heads;
+  w.h = (bg % p.kv_heads) * group + hh;
+  const int qb = p.causal && !p.window ? ((k & 1) ? k >> 1 : nb - 1 - (k >> 1)) : k;
+  w.r0 = qb * WIN_ROWS;
+  return w;
+}
+
+// a wave's transposed result (rows: columns of the head, lane: its query) times `mul` of the lane through its own piece of LDS to rows;
+// rows at and behind `len` are written as zero
+template <typename T, int DH>
+__device__ __forceinline__ void win_store_rows(unsigned char *lds, int wave, const f32x16 (&acc)[DH / 32], float mul, int q0, int len, int seq,
+                                               int dh, GPP_G void *out, int64_t row0, int64_t ld, GPP_G void *out2, int64_t ld2, int64_t col0) {
+  constexpr int ST = DH * (int)sizeof(T) + 16, EPC = 16 / sizeof(T);
+  unsigned char *stage = lds + wave * 32 * ST;
+  const int l = threadIdx.x & 63;
+#pragma unroll
+  for (int d = 0; d < DH / 32; ++d)
+#pragma unroll
+    for (int r = 0; r < 16; r += 4) {
+      T v[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if constexpr (sizeof(T) == 2) v[e] = f32_to_bf16_bits(acc[d][r + e] * mul);
+        else v[e] = acc[d][r + e] * mul;
+      }
+      __builtin_memcpy(stage + (l & 31) * ST + (32 * d + win_acc_row(r)) * sizeof(T), v, sizeof(v));
+    }
+  __builtin_amdgcn_wave_barrier();
+  const int cpr = dh / EPC;
+  for (int c = l; c < 32 * (DH / EPC); c += 64) {
+    const int row = c / (DH / EPC), k = c % (DH / EPC), q = q0 + row;
+    if (k >= cpr || q >= seq) continue;
+    u32x4 v = *(const u32x4 *)(stage + row * ST + k * 16);
+    if (q >= len) v = (u32x4){0u, 0u, 0u, 0u};
+    if (out) *(GPP_G u32x4 *)((GPP_G T *)out + (row0 + q) * ld + col0 + k * EPC) = v;
+    if (out2) *(GPP_G u32x4 *)((GPP_G T *)out2 + (row0 + q) * ld2 + col0 + k * EPC) = v;
+  }
+}
+
+// ======================================================================= forward
+template <typename T, int DH>
+__global__ __launch_bounds__(256, 2) void k_window_fwd_mfma(const WindowProb *__restrict__ probs, int n, ExtPtrs ext, StageFlags *flags) {
+  typedef WinTile<T, DH> C;
+  typedef WinFrag<T> F;
+  __shared__ __attribute__((aligned(16))) unsigned char lds[4 * C::BYTES > 128 * (DH * C::ES + 16) ? 4 * C::BYTES : 128 * (DH * C::ES + 16)];
+  const int bid = big_spread(gridDim.x);
+  const int pi = find_prob(probs, n, bid);
+  const WindowProb p = probs[pi];
+  const WinBlock w = win_query_block(p, bid - p.blk_begin);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int len = __builtin_amdgcn_readfirstlane(window_length_checked(p, ext, w.b, w.h == 0 && w.r0 == 0 && threadIdx.x == 0, flags));
+  const GPP_G T *qkv = (const GPP_G T *)(p.ext_qkv >= 0 ? ext.p[p.ext_qkv] : p.qkv);
+  const int64_t row0 = (int64_t)w.b * p.seq;
+  const int kh = w.h / (p.heads / p.kv_heads);
+  const GPP_G T *kbase = qkv + row0 * p.ld_qkv + (int64_t)(p.heads + kh) * p.dh, *vbase = kbase + (int64_t)p.kv_heads * p.dh;
+  const int q0 = w.r0 + 32 * wave, q = q0 + (lane & 31), qc = max(0, min(q, len - 1));
+  const WinRange tiles = win_range<C::KT>(p, w.r0, min(w.r0 + WIN_ROWS, len) - 1, len);
+  const WinWave mine = win_wave(p, q0, len);
+  const WindowKeys keys = window_keys(p, qc, len);
+  const float scale2 = p.scale * LOG2E;
+
+  const WinCopy<T, DH, 4> co = win_copy_offsets<T, DH, 4>(wave, p.ld_qkv, p.dh);
+  const uint32_t lds0 = lds_address((const uint16_t *)lds);
+  auto copy = [&](int t, int buf) {
+    const int k0 = tiles.tile(t) * C::KT;
+    const uint32_t bytes = win_tile_bytes(min(C::KT, len - k0), p.ld_qkv, p.dh, C::ES);
+    rsrc4 rk = win_rsrc(kbase + (int64_t)k0 * p.ld_qkv, bytes), rv = win_rsrc(vbase + (int64_t)k0 * p.ld_qkv, bytes);
+    settle(rk, rv);
+    win_copy(rk, co, lds0 + 2 * buf * C::BYTES, wave);
+    win_copy(rv, co, lds0 + (2 * buf + 1) * C::BYTES, wave);
+  };
+  if (tiles.n > 0) copy(0, 0);
+  const WinLane<T, DH> at = win_lane<T, DH>();
+  const WinRows<T, DH> qf = win_rows<T, DH>(qkv, row0 + qc, p.ld_qkv, (int64_t)w.h * p.dh, p.dh);
+  f32x16 o[C::DB];
+#pragma unroll
+  for (int d = 0; d < C::DB; ++d) o[d] = win_zero();
+  float m = -INFINITY, l = 0.0f;     // running maximum (base 2, the same in a lane and its partner) and this lane's share of the sum
+
+  for (int t = 0; t < tiles.n; ++t) {
+    const int cur = t & 1;
+    copies_landed_barrier<0>();
+    if (t + 1 < tiles.n) copy(t + 1, cur ^ 1);
+    const unsigned char *tk = lds + 2 * cur * C::BYTES, *tv = tk + C::BYTES;
+    const int k0 = tiles.tile(t) * C::KT, sees = mine.sees(k0, C::KT);
+    if (sees == WIN_NONE) continue;
+    f32x16 st[C::SUB];
+#pragma unroll
+    for (int u = 0; u < C::SUB; ++u) {
+      st[u] = win_zero();
+#pragma unroll
+      for (int s = 0; s < C::KS; ++s) st[u] = F::mma(win_row_frag<T, DH>(at, tk, 32 * u, s), qf.f[s], st[u]);
+    }
+    if (sees == WIN_SOME) {
+      asm volatile("");      // keeps this a branch
+      const int a = k0 - keys.first, span = keys.end - keys.first, sk = keys.sink_end - k0;
+#pragma unroll
+      for (int u = 0; u < C::SUB; ++u)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int j = 32 * u + win_acc_row(r);
+          if (!((unsigned)(a + j) < (unsigned)span || j < sk)) st[u][r] = -INFINITY;
+        }
+    }
+    float mx = st[0][0];
+#pragma unroll
+    for (int u = 0; u < C::SUB; ++u)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) mx = fmaxf(mx, st[u][r]);
+    const float m_tile = win_half_max(mx) * scale2;
+    // The maximum only keeps the exponentials in range: it follows where it grew by more than 2^8, which spares most tiles the
+    // rescaling of the output
+    if (__ballot(m_tile > m + 8.0f) != 0ull) {
+      const float m_new = fmaxf(m, m_tile), ref = m_new == -INFINITY ? 0.0f : m_new;
+      const float alpha = __builtin_amdgcn_exp2f(m - ref);
+      l *= alpha;
+#pragma unroll
+      for (int d = 0; d < C::DB; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[d][r] *= alpha;
+      m = m_new;
+    }
+    const float ref = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+    for (int u = 0; u < C::SUB; ++u)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        st[u][r] = __builtin_amdgcn_exp2f(fmaf(st[u][r], scale2, -ref));
+        l += st[u][r];
+      }
+#pragma unroll
+    for (int c = 0; c < 2 * C::SUB; ++c) {
+      const typename F::type pf = F::pack(st[c >> 1], c & 1);
+#pragma unroll
+      for (int d = 0; d < C::DB; ++d) o[d] = F::mma(win_col_frag<T, DH>(at, tv, 16 * c, d), pf, o[d]);
+    }
+  }
+  __syncthreads();
+  l = win_half_sum(l);
+  if (p.lse && lane < 32 && q < len) p.lse[((int64_t)w.b * p.heads + w.h) * p.seq + q] = m + __builtin_amdgcn_logf(l);
+  win_store_rows<T, DH>(lds, wave, o, 1.0f / l, q0, len, p.seq, p.dh, p.out, row0, p.ld_out, p.ext_out >= 0 ? (GPP_G void *)ext.p[p.ext_out] : nullptr,
+                        p.ld_ext, (int64_t)w.h * p.dh);
+}
+
+// ======================================================================= backward: dQ, and delta = rowsum(dO * O)
+template <typename T, int DH>
+__global__ __launch_bounds__(256, 2) void k_window_dq_mfma(const WindowProb *__restrict__ probs, int n, ExtPtrs ext) {
+  typedef WinTile<T, DH> C;
+  typedef WinFrag<T> F;
+  __shared__ __attribute__((aligned(16))) unsigned char lds[4 * C::BYTES > 128 * (DH * C::ES + 16) ? 4 * C::BYTES : 128 * (DH * C::ES + 16)];
+  const int bid = big_spread(gridDim.x);
+  const int pi = find_prob(probs, n, bid);
+  const WindowProb p = probs[pi];
+  const WinBlock w = win_query_block(p, bid - p.blk_begin);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int len = __builtin_amdgcn_readfirstlane(window_length(p, w.b));
+  const GPP_G T *qkv = (const GPP_G T *)p.qkv;
+  const int64_t row0 = (int64_t)w.b * p.seq;
+  const int kh = w.h / (p.heads / p.kv_heads);
+  const GPP_G T *kbase = qkv + row0 * p.ld_qkv + (int64_t)(p.heads + kh) * p.dh, *vbase = kbase + (int64_t)p.kv_heads * p.dh;
+  const int q0 = w.r0 + 32 * wave, q = q0 + (lane & 31), qc = max(0, min(q, len - 1));
+  const WinRange tiles = win_range<C::KT>(p, w.r0, min(w.r0 + WIN_ROWS, len) - 1, len);
+  const WinWave mine = win_wave(p, q0, len);
+  WindowKeys keys = window_keys(p, qc, len);
+  if (keys.count == 1) keys.end = keys.first = keys.sink_end = 0;      // a single key's probability is constant: no gradient
+  const float scale2 = p.scale * LOG2E;
+  const int64_t stat = ((int64_t)w.b * p.heads + w.h) * p.seq + qc;
+
+  const WinCopy<T, DH, 4> co = win_copy_offsets<T, DH, 4>(wave, p.ld_qkv, p.dh);
+  const uint32_t lds0 = lds_address((const uint16_t *)lds);
+  auto copy = [&](int t, int buf) {
+    const int k0 = tiles.tile(t) * C::KT;
+    const uint32_t bytes = win_tile_bytes(min(C::KT, len - k0), p.ld_qkv, p.dh, C::ES);
+    rsrc4 rk = win_rsrc(kbase + (int64_t)k0 * p.ld_qkv, bytes), rv = win_rsrc(vbase + (int64_t)k0 * p.ld_qkv, bytes);
+    settle(rk, rv);
+    win_copy(rk, co, lds0 + 2 * buf * C::BYTES, wave);
+    win_copy(rv, co, lds0 + (2 * buf + 1) * C::BYTES, wave);
+  };
+  GPP_G void *dqkv = p.ext_out >= 0 ? (GPP_G void *)ext.p[p.ext_out] : p.out;
+  const int nt = dqkv ? tiles.n : 0;
+  if (nt > 0) copy(0, 0);
+  const WinLane<T, DH> at = win_lane<T, DH>();
+  const WinRows<T, DH> qf = win_rows<T, DH>(qkv, row0 + qc, p.ld_qkv, (int64_t)w.h * p.dh, p.dh);
+  const WinRows<T, DH> gf = win_rows<T, DH>(p.ext_dout >= 0 ? ext.p[p.ext_dout] : p.dout, row0 + qc, p.ld_dout, (int64_t)w.h * p.dh, p.dh);
+  float delta = 0.0f;
+  {
+    const WinRows<T, DH> of = win_rows<T, DH>(p.o, row0 + qc, p.ld_o, (int64_t)w.h * p.dh, p.dh);
+#pragma unroll
+    for (int s = 0; s < C::KS; ++s)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) delta = fmaf(F::get(gf.f[s], e), F::get(of.f[s], e), delta);
+    delta = win_half_sum(delta);
+    if (lane < 32 && q < len) p.delta[stat] = delta;
+  }
+  const float lse = q0 < len ? p.lse[stat] : 0.0f;
+  f32x16 dq[C::DB];
+#pragma unroll
+  for (int d = 0; d < C::DB; ++d) dq[d] = win_zero();
+
+  for (int t = 0; t < nt; ++t) {
+    const int cur = t & 1;
+    copies_landed_barrier<0>();
+    if (t + 1 < nt) copy(t + 1, cur ^ 1);
+    const unsigned char *tk = lds + 2 * cur * C::BYTES, *tv = tk + C::BYTES;
+    const int k0 = tiles.tile(t) * C::KT, sees = mine.sees(k0, C::KT);
+    if (sees == WIN_NONE) continue;
+#pragma unroll
+    for (int u = 0; u < C::SUB; ++u) {
+      f32x16 st = win_zero(), dp = win_zero();
+#pragma unroll
+      for (int s = 0; s < C::KS; ++s) {
+        st = F::mma(win_row_frag<T, DH>(at, tk, 32 * u, s), qf.f[s], st);
+        dp = F::mma(win_row_frag<T, DH>(at, tv, 32 * u, s), gf.f[s], dp);
+      }
+#pragma unroll
+      for (int r = 0; r < 16; ++r) st[r] = __builtin_amdgcn_exp2f(fmaf(st[r], scale2, -lse)) * (dp[r] - delta);
+      if (sees == WIN_SOME) {
+        asm volatile("");
+        const int a = k0 - keys.first, span = keys.end - keys.first, sk = keys.sink_end - k0;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int j = 32 * u + win_acc_row(r);
+          if (!((unsigned)(a + j) < (unsigned)span || j < sk)) st[r] = 0.0f;
+        }
+      }
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        const typename F::type sf = F::pack(st, c);
+#pragma unroll
+        for (int d = 0; d < C::DB; ++d) dq[d] = F::mma(win_col_frag<T, DH>(at, tk, 32 * u + 16 * c, d), sf, dq[d]);
+      }
+    }
+  }
+  if (!dqkv) return;
+  __syncthreads();
+  win_store_rows<T, DH>(lds, wave, dq, p.scale, q0, len, p.seq, p.dh, dqkv, row0, p.ld_out, nullptr, 0, (int64_t)w.h * p.dh);
+}
+
+// ======================================================================= backward: dK, dV
+// The steps of a block of keys are the tiles of queries that see one of them, for every query head that shares the keys, head by
+// head.  A block's steps go to one workgroup, or `parts` of at most `part_steps` to several, whose fp32 sums k_window_join adds in
+// order.  Units of work: the first `whole` blocks unsplit, the other blocks part by part, then the blocks of the first
+// tokens, which every query sees, part by part.
+struct WinUnit {
+  int b, g, c0, part;        // sample, key / value head, first key, part or -1: unsplit
+  int slot;                  // of the parts of the launch
+};
+__device__ __forceinline__ WinUnit win_unit(const WindowProb &p, int idx) {
+  const int nb = (p.seq + WIN_ROWS - 1) / WIN_ROWS, nr = nb - p.sink_blocks, blocks = p.batch * p.kv_heads * nr;
+  WinUnit w;
+  w.slot = idx - p.whole;
+  w.part = -1;
+  int block, c;
+  if (idx < p.whole || w.slot < (blocks - p.whole) * p.parts) {
+    block = idx < p.whole ? idx : p.whole + w.slot / p.parts;
+    if (idx >= p.whole && p.parts > 1) w.part = w.slot % p.parts;
+    c = p.sink_blocks + block % nr;
+    block /= nr;
+  } else {
+    const int k = w.slot - (blocks - p.whole) * p.parts;
+    block = k / p.sink_parts;
+    if (p.sink_parts > 1) w.part = k % p.sink_parts;
+    c = block % p.sink_blocks;
+    block /= p.sink_blocks;
+  }
+  w.b = block / p.kv_heads;
+  w.g = block % p.kv_heads;
+  w.c0 = c * WIN_ROWS;
+  return w;
+}
+struct WinSteps {
+  int t0, nt, n;             // first tile of queries, tiles per head, steps in all
+};
+template <int KT>
+__device__ __forceinline__ WinSteps win_steps(const WindowProb &p, int c0, int len) {
+  WinSteps w = {0, 0, 0};
+  if (c0 < len) {
+    const int first = window_queries(p, c0, len).first;
+    const int end = c0 < p.sinks ? len : window_queries(p, min(c0 + WIN_ROWS, len) - 1, len).end;
+    w.t0 = first / KT;
+    w.nt = (end - 1) / KT - w.t0 + 1;
+    w.n = w.nt * (p.heads / p.kv_heads);
+  }
+  return w;
+}
+
+// A wave owns 32 keys and, where a tile holds 64 queries, one half of them: the two waves of a SIMD that share their keys hide each
+// other's chains (LDS reads -> score products -> exponentials -> gradient products), and add their sums at the end.  Two waves have 256
+// registers each; with heads of more than 64 columns the sums take 128 of them, so V is then read from LDS like the tiles, K stays
+// in registers.
+template <typename T, int DH>
+struct WinKeyCfg {
+  typedef WinTile<T, DH> C;
+  static constexpr int QG = C::SUB, NW = 4 * QG, BUF = 2 * C::BYTES + 1024;      // Q, dO, and the log-sum-exps and deltas of the tile's queries
+  static constexpr bool V_LDS = sizeof(T) == 2 && DH > 64;
+  static constexpr int V_BYTES = V_LDS ? WIN_ROWS / C::RPG * C::GROUP : 0, ST = DH * C::ES + 16;
+  static constexpr int JOIN = QG > 1 ? 4 * 32 * DH * 4 : 0, OUT = 4 * 32 * ST;    // over the tiles: a sum of four waves, rows of the result
+  static constexpr int TILES = 2 * BUF + V_BYTES, LDS = TILES > JOIN ? (TILES > OUT ? TILES : OUT) : (JOIN > OUT ? JOIN : OUT);
+};
+
+template <typename T, int DH>
+__global__ __launch_bounds__((WinKeyCfg<T, DH>::NW * 64), (DH * sizeof(T) <= 256 ? 2 : 1)) void k_window_dkv_mfma(const WindowProb *__restrict__ probs, int n,
+                                                                                                       ExtPtrs ext) {
+  typedef WinTile<T, DH> C;
+  typedef WinFrag<T> F;
+  typedef WinKeyCfg<T, DH> K;
+  __shared__ __attribute__((aligned(16))) unsigned char lds[K::LDS];
+  const int pi = find_prob(probs, n, blockIdx.x);
+  const WindowProb p = probs[pi];
+  GPP_G void *dqkv = p.ext_out >= 0 ? (GPP_G void *)ext.p[p.ext_out] : p.out;
+  if (!dqkv) return;
+  // (an XCD takes a run of neighbouring units: of the unsplit ones and of the others)
+  const int local = blockIdx.x - p.blk_begin;
+  const WinUnit w = win_unit(p, local < p.whole ? win_spread(local, p.whole) : p.whole + win_spread(local - p.whole, p.units - p.whole));
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), kg = wave & 3, qg = wave >> 2;
+  const int len = __builtin_amdgcn_readfirstlane(window_length(p, w.b));
+  const WinSteps st_ = win_steps<C::KT>(p, w.c0, len);
+  const bool split = w.part >= 0;
+  const int s0 = __builtin_amdgcn_readfirstlane(split ? w.part * p.part_steps : 0);
+  const int s1 = __builtin_amdgcn_readfirstlane(split ? min(st_.n, s0 + p.part_steps) : st_.n);
+  const int nt = __builtin_amdgcn_readfirstlane(st_.nt), t0 = __builtin_amdgcn_readfirstlane(st_.t0);
+  if (split && s0 >= s1) return;                // (such a part is not added)
+  const GPP_G T *qkv = (const GPP_G T *)p.qkv, *dout = (const GPP_G T *)(p.ext_dout >= 0 ? ext.p[p.ext_dout] : p.dout);
+  const int64_t row0 = (int64_t)w.b * p.seq;
+  const int group = p.heads / p.kv_heads, h0 = w.g * group;
+  const int k0 = w.c0 + 32 * kg, k1 = min(k0 + 31, len - 1), kc = max(0, min(k0 + (lane & 31), len - 1));
+  const int64_t kcol = (int64_t)(p.heads + w.g) * p.dh, vcol = kcol + (int64_t)p.kv_heads * p.dh;
+  const WindowQueries seen = window_queries(p, kc, len);
+  const int win = (int)min(p.window ? p.window : (int64_t)p.seq, (int64_t)p.seq), nsink = (int)min(p.sinks, (int64_t)p.seq);
+  // queries that see one key only have no gradient of their score: all of them, or the first
+  const bool all_single = (win == 1 && nsink == 0) || len == 1, first_single = p.causal || (win == 1 && min(nsink, len) <= 1);
+  const float scale2 = p.scale * LOG2E;
+
+  const WinCopy<T, DH, K::NW> cq = win_copy_offsets<T, DH, K::NW>(wave, p.ld_qkv, p.dh), cg = win_copy_offsets<T, DH, K::NW>(wave, p.ld_dout, p.dh);
+  const uint32_t lds0 = lds_address((const uint16_t *)lds);
+  int head = s0 < s1 ? s0 / nt : 0, tile = s0 - head * nt;      // of the next step to be copied
+  auto copy_next = [&](int buf) {
+    const int h = h0 + head, i0 = (t0 + tile) * C::KT, rows = min(C::KT, len - i0);
+    rsrc4 rq = win_rsrc(qkv + (row0 + i0) * p.ld_qkv + (int64_t)h * p.dh, win_tile_bytes(rows, p.ld_qkv, p.dh, C::ES));
+    rsrc4 rg = win_rsrc(dout + (row0 + i0) * p.ld_dout + (int64_t)h * p.dh, win_tile_bytes(rows, p.ld_dout, p.dh, C::ES));
+    settle(rq, rg);
+    win_copy(rq, cq, lds0 + buf * K::BUF, wave);
+    win_copy(rg, cg, lds0 + buf * K::BUF + C::BYTES, wave);
+    if (wave < 2) {      // one wave the log-sum-exps, one the deltas (queries behind the end: zero, as their rows)
+      const int64_t stat = ((int64_t)w.b * p.heads + h) * p.seq + i0;
+      rsrc4 rs = win_rsrc((wave ? p.delta : p.lse) + stat, (uint32_t)max(rows, 0) * 4), same = rs;
+      settle(rs, same);
+      lds_copy4(rs, lds0 + buf * K::BUF + 2 * C::BYTES + wave * 512, lane * 4);
+    }
+    if (++tile == nt) {
+      tile = 0;
+      ++head;
+    }
+  };
+  int now = tile;       // of the step that is being multiplied
+  if (s0 < s1) {
+    copy_next(0);
+    if constexpr (K::V_LDS) {      // 128 rows of V: two tiles' worth
+      const WinCopy<T, DH, K::NW> cv = win_copy_offsets<T, DH, K::NW>(wave, p.ld_qkv, p.dh);
+#pragma unroll
+      for (int half = 0; half < WIN_ROWS / C::KT; ++half) {
+        const int r0 = w.c0 + half * C::KT;
+        rsrc4 rv = win_rsrc(qkv + (row0 + min(r0, len - 1)) * p.ld_qkv + vcol, win_tile_bytes(min(C::KT, len - r0), p.ld_qkv, p.dh, C::ES)), same = rv;
+        settle(rv, same);
+        win_copy(rv, cv, lds0 + 2 * K::BUF + half * C::BYTES, wave);
+      }
+    }
+  }
+  const WinLane<T, DH> at = win_lane<T, DH>();
+  const WinRows<T, DH> kf = win_rows<T, DH>(qkv, row0 + kc, p.ld_qkv, kcol, p.dh);
+  WinRows<T, DH> vf;
+  if constexpr (!K::V_LDS) vf = win_rows<T, DH>(qkv, row0 + kc, p.ld_qkv, vcol, p.dh);
+  f32x16 dk[C::DB], dv[C::DB];
+#pragma unroll
+  for (int d = 0; d < C::DB; ++d) dk[d] = dv[d] = win_zero();
+
+  for (int s = s0; s < s1; ++s) {
+    const int cur = (s - s0) & 1;
+    copies_landed_barrier<0>();
+    if (s + 1 < s1) copy_next(cur ^ 1);
+    const unsigned char *tq = lds + cur * K::BUF, *tg = tq + C::BYTES;
+    const int i0 = (t0 + now) * C::KT + 32 * qg, i1 = min(i0 + 31, len - 1);
+    now = now + 1 == nt ? 0 : now + 1;
+    if (k0 >= len || i0 >= len || (p.causal && i1 < k0) || !(k0 < nsink || (i0 - k1 < win && k0 - i1 < win))) continue;
+    const bool all = (!p.causal || k1 <= i0) && (k1 < nsink || (i1 - k0 < win && k1 - i0 < win));
+    const float *tl = (const float *)(tq + 2 * C::BYTES) + 32 * qg + 4 * (lane >> 5), *td = tl + 128;
+    f32x16 st = win_zero(), dp = win_zero();
+#pragma unroll
+    for (int x = 0; x < C::KS; ++x) {
+      st = F::mma(win_row_frag<T, DH>(at, tq + C::at(32) * qg, 0, x), kf.f[x], st);
+      if constexpr (K::V_LDS) dp = F::mma(win_row_frag<T, DH>(at, tg + C::at(32) * qg, 0, x), win_row_frag<T, DH>(at, lds + 2 * K::BUF + C::at(32) * kg, 0, x), dp);
+      else dp = F::mma(win_row_frag<T, DH>(at, tg + C::at(32) * qg, 0, x), vf.f[x], dp);
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const f32x4 lse = *(const f32x4 *)(tl + 8 * k), delta = *(const f32x4 *)(td + 8 * k);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int r = 4 * k + e;
+        st[r] = __builtin_amdgcn_exp2f(fmaf(st[r], scale2, -lse[e]));
+        dp[r] = st[r] * (dp[r] - delta[e]);
+      }
+    }
+    if (!all) {
+      asm volatile("");      // keeps this a branch
+      const int a = i0 - seen.first, span = seen.end - seen.first;
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        if (!((unsigned)(a + win_acc_row(r)) < (unsigned)span)) st[r] = dp[r] = 0.0f;
+      if (i0 == 0 && first_single && lane < 32) dp[0] = 0.0f;
+    }
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      const typename F::type pf = F::pack(st, c), sf = F::pack(dp, c);
+#pragma unroll
+      for (int d = 0; d < C::DB; ++d) {
+        dv[d] = F::mma(pf, win_col_frag<T, DH>(at, tg + C::at(32) * qg, 16 * c, d), dv[d]);
+        dk[d] = F::mma(sf, win_col_frag<T, DH>(at, tq + C::at(32) * qg, 16 * c, d), dk[d]);
+      }
+    }
+  }
+  __syncthreads();
+  if constexpr (K::QG > 1) {      // the second half's sums to the first half's waves, dK and then dV
+    float *sums = (float *)lds + kg * 32 * DH + lane;
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+      f32x16(&acc)[C::DB] = which ? dv : dk;
+      if (qg == 1) {
+#pragma unroll
+        for (int d = 0; d < C::DB; ++d)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) sums[(d * 16 + r) * 64] = acc[d][r];
+      }
+      __syncthreads();
+      if (qg == 0) {
+#pragma unroll
+        for (int d = 0; d < C::DB; ++d)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) acc[d][r] += sums[(d * 16 + r) * 64];
+      }
+      __syncthreads();
+    }
+    if (qg == 1) return;
+  }
+  const float mk = all_single ? 0.0f : p.scale;
+  if (split) {     // [part of the launch][dK, dV][key][column] in fp32
+    GPP_G float *part = p.partial + (int64_t)w.slot * 2 * WIN_ROWS * DH + (int64_t)(32 * kg) * DH + (lane & 31);
+#pragma unroll
+    for (int d = 0; d < C::DB; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        part[win_acc_row(r) * DH + 32 * d] = dk[d][r] * mk;
+        part[(WIN_ROWS + win_acc_row(r)) * DH + 32 * d] = dv[d][r];
+      }
+    return;
+  }
+  // each wave turns its two blocks of 32 keys in its own piece of LDS, one after the other, and writes whole pieces of rows
+  unsigned char *stage = lds + kg * 32 * K::ST;
+#pragma unroll
+  for (int which = 0; which < 2; ++which) {
+#pragma unroll
+    for (int d = 0; d < C::DB; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        T *to = (T *)(stage + win_acc_row(r) * K::ST) + 32 * d + (lane & 31);
+        const float v = which ? dv[d][r] : dk[d][r] * mk;
+        if constexpr (sizeof(T) == 2) *to = f32_to_bf16_bits(v);
+        else *to = v;
+      }
+    __builtin_amdgcn_wave_barrier();
+    for (int c = lane; c < 32 * (DH / C::EPC); c += 64) {
+      const int row = c / (DH / C::EPC), k = c % (DH / C::EPC);
+      if (k * C::EPC >= p.dh || k0 + row >= p.seq) continue;
+      u32x4 v = *(const u32x4 *)(stage + row * K::ST + k * 16);
+      if (k0 + row >= len) v = (u32x4){0u, 0u, 0u, 0u};
+      *(GPP_G u32x4 *)((GPP_G T *)dqkv + (row0 + k0 + row) * p.ld_out + (which ? vcol : kcol) + k * C::EPC) = v;
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
+// The sums of a split block's parts, in order: four columns of a key per thread, DH / 4 workgroups per block
+template <typename T, int DH>
+__global__ __launch_bounds__(256) void k_window_join(const WindowProb *__restrict__ probs, int n, ExtPtrs ext) {
+  typedef WinTile<T, DH> C;
+  const int pi = find_prob(probs, n, blockIdx.x);
+  const WindowProb p = probs[pi];
+  GPP_G T *dqkv = (GPP_G T *)(p.ext_out >= 0 ? ext.p[p.ext_out] : p.out);
+  if (!dqkv) return;
+  const int nb = (p.seq + WIN_ROWS - 1) / WIN_ROWS, rest = p.batch * p.kv_heads * (nb - p.sink_blocks) - p.whole;
+  const int regular = p.parts > 1 ? rest : 0;                     // split blocks that hold no first token
+  const int blk = (blockIdx.x - p.blk_begin) / (DH / 4), piece = (blockIdx.x - p.blk_begin) % (DH / 4);
+  const WinUnit w = win_unit(p, p.whole + (blk < regular ? blk * p.parts : rest * p.parts + (blk - regular) * p.sink_parts));
+  const int first = w.slot, len = window_length(p, w.b);
+  const int parts = (win_steps<C::KT>(p, w.c0, len).n + p.part_steps - 1) / p.part_steps;
+  const int64_t row0 = (int64_t)w.b * p.seq, kcol = (int64_t)(p.heads + w.g) * p.dh, vcol = kcol + (int64_t)p.kv_heads * p.dh;
+  const int u = piece * 256 + threadIdx.x, c = u % (DH / 4) * 4, row = u / (DH / 4) % WIN_ROWS, which = u / (DH / 4) / WIN_ROWS, key = w.c0 + row;
+  if (key >= p.seq || c >= p.dh) return;
+  f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
+  if (key < len) {
+    const GPP_G float *at = p.partial + ((int64_t)first * 2 + which) * WIN_ROWS * DH + (int64_t)row * DH + c;
+#pragma unroll 8
+    for (int k = 0; k < parts; ++k) sum += *(const GPP_G f32x4 *)(at + (int64_t)k * 2 * WIN_ROWS * DH);
+  }
+  T v[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    if constexpr (sizeof(T) == 2) v[e] = f32_to_bf16_bits(sum[e]);
+    else v[e] = sum[e];
+  }
+  GPP_G T *to = dqkv + (row0 + key) * p.ld_out + (which ? vcol : kcol) + c;
+  if constexpr (sizeof(T) == 2) {
+    typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+    u32x2 w2;
+    __builtin_memcpy(&w2, v, 8);
+    *(GPP_G u32x2 *)to = w2;
+  } else {
+    u32x4 w4;
+    __builtin_memcpy(&w4, v, 16);
+    *(GPP_G u32x4 *)to = w4;
+  }
+}
+
+// ---- host ------------------------------------------------------------------------------------------------
+// template head dimension of a record, or 0: the row-parallel kernels
+int window_mfma_dh(const WindowProb &p) {
+  const int es = p.dtype == DT_BF16 ? 2 : 4, epc = 16 / es;
+  if (p.dtype == DT_I32 || p.out_dtype != p.dtype || p.dh > 128 || p.dh % epc) return 0;
+  if ((p.ld_qkv | p.ld_out | p.ld_o | p.ld_dout | p.ld_ext) % epc) return 0;
+  if (((uintptr_t)p.qkv | (uintptr_t)p.out | (uintptr_t)p.o | (uintptr_t)p.dout) & 15) return 0;
+  if ((p.ld_qkv | p.ld_dout) >= (1ll << 24)) return 0;        // a tile's offsets stay far inside 32 bits
+  return p.dh <= 32 ? 32 : (p.dh <= 64 ? 64 : (p.dh <= 96 ? 96 : 128));
+}
+int window_mfma_query_blocks(const WindowProb &p) { return p.batch * p.heads * ((p.seq + WIN_ROWS - 1) / WIN_ROWS); }
+static int window_tile_rows(const WindowProb &p, int dh) { return dh * (p.dtype == DT_BF16 ? 2 : 4) > 256 ? 32 : 64; }
+
+// Cuts the key blocks of a launch (see WinUnit) into units, of which `slots` run at once: the first `whole` blocks stay in one piece,
+// the others and the blocks of the first tokens, which take several times as long, go in parts of part_steps steps, which fill the
+// gaps that whole blocks leave.  Of the pairs (whole, part_steps) the one with the least estimate, in steps: what a slot has to do, but
+// no less than the rounds of whole blocks, plus half a part of unevenness; a unit costs four steps for its operands and its
+// result, a part its sums' way through memory, the joining launch a few steps.
+void window_plan_parts(WindowProb &p, int dh, int slots) {
+  const int64_t kt = window_tile_rows(p, dh), group = p.heads / p.kv_heads, seq = p.seq, nb = (seq + WIN_ROWS - 1) / WIN_ROWS;
+  const int64_t win = p.window ? std::min<int64_t>(p.window, seq) : seq, bg = (int64_t)p.batch * p.kv_heads;
+  const int64_t sb = p.window ? (std::min<int64_t>(p.sinks, seq) + WIN_ROWS - 1) / WIN_ROWS : 0;
+  auto tiles = [&](int64_t queries) { return std::min<int64_t>((std::min(queries, seq) + kt - 1) / kt + 1, (seq + kt - 1) / kt); };
+  const int64_t regular = group * tiles(WIN_ROWS - 1 + (p.causal ? win : 2 * win - 1)), every = group * tiles(seq), blocks = bg * (nb - sb);
+  const bool triangle = p.causal && !p.window;       // half of the steps of a regular block, on average; the first blocks have most
+  auto up = [](int64_t v, int64_t by) { return (v + by - 1) / by; };
+  double best = 1e300;
+  for (int64_t whole = blocks;; whole = std::max<int64_t>(0, std::min(whole - 1, whole - slots / 8) / 8 * 8)) {
+    for (int64_t part = 8; part < 2 * every + 8; part += part < 32 ? 4 : part / 8) {
+      const int64_t rest = blocks - whole, parts = up(regular, part), sink_parts = sb ? up(every, part) : 1;
+      const int64_t split = (parts > 1 ? rest * parts : 0) + (sink_parts > 1 ? bg * sb * sink_parts : 0);
+      const int64_t units = whole + rest * parts + bg * sb * sink_parts;
+      const double steps = (double)blocks * regular * (triangle ? 0.5 : 1.0) + (double)(bg * sb * every);
+      const double slot = (steps + 4.0 * (double)units) / slots;
+      const double longest = std::max((double)(whole ? regular : 0), (double)std::min(part, std::max(rest ? regular : 0, sb ? every : 0))) + 4.0;
+      const double rounds = triangle ? longest : (double)up(whole, slots) * (regular + 4.0);
+      const double t = std::max(std::max(slot, longest), rounds) + 0.5 * (split ? (double)part : 0.0) + (split ? 6.0 + 0.00035 * dh * (double)split : 0.0);
+      if (t >= best) continue;
+      best = t;
+      p.whole = (int32_t)whole;
+      p.part_steps = (int32_t)part;
+      p.parts = (int32_t)parts;
+      p.sink_parts = (int32_t)sink_parts;
+      p.units = (int32_t)units;
+    }
+    if (whole == 0) break;
+  }
+  p.sink_blocks = (int32_t)sb;
+}
+int window_mfma_key_blocks(const WindowProb &p) { return p.units; }
+int window_join_blocks(const WindowProb &p, int dh) {
+  const int64_t nb = (p.seq + WIN_ROWS - 1) / WIN_ROWS, bg = (int64_t)p.batch * p.kv_heads, sb = p.sink_blocks;
+  return (int)(dh / 4 * ((p.parts > 1 ? bg * (nb - sb) - p.whole : 0) + (p.sink_parts > 1 ? bg * sb : 0)));
+}
+int64_t window_partial_bytes(const WindowProb &p, int dh) {
+  return window_join_blocks(p, dh) ? (int64_t)(p.units - p.whole) * 2 * WIN_ROWS * dh * 4 : 0;
+}
+// workgroups of the dK / dV kernel that run at once: two waves per SIMD have the registers, four with heads of 32 columns in bf16
+int window_key_slots(int dtype, int dh) { return dtype == DT_BF16 && dh == 32 ? 512 : 256; }
+
+#define WIN_GO(KERNEL, ...)                                                                                       \
+  do {                                                                                                            \
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(total_blocks), dim3(256), 0, s, __VA_ARGS__); }; \
+    if (total_blocks <= 0) break;                                                                                 \
+    if (dtype == DT_BF16) {                                                                                       \
+      if (dh == 32) go(KERNEL<uint16_t, 32>);                                                                     \
+      else if (dh == 64) go(KERNEL<uint16_t, 64>);                                                                \
+      else if (dh == 96) go(KERNEL<uint16_t, 96>);                                                                \
+      else go(KERNEL<uint16_t, 128>);                                                                             \
+    } else {                                                                                                      \
+      if (dh == 32) go(KERNEL<float, 32>);                                                                        \
+      else if (dh == 64) go(KERNEL<float, 64>);                                                                   \
+      else if (dh == 96) go(KERNEL<float, 96>);                                                                   \
+      else go(KERNEL<float, 128>);                                                                                \
+    }                                                                                                             \
+  } while (0)
+
+void launch_window_fwd_mfma(const WindowProb *probs, int n, int total_blocks, int dtype, int dh, const ExtPtrs &ext, StageFlags *flags, hipStream_t s) {
+  WIN_GO(k_window_fwd_mfma, probs, n, ext, flags);
+}
+void launch_window_dq_mfma(const WindowProb *probs, int n, int total_blocks, int dtype, int dh, const ExtPtrs &ext, hipStream_t s) {
+  WIN_GO(k_window_dq_mfma, probs, n, ext);
+}
+void launch_window_dkv_mfma(const WindowProb *probs, int n, int total_blocks, int dtype, int dh, const ExtPtrs &ext, hipStream_t s) {
+  if (total_blocks <= 0) return;
+  auto go = [&](auto kernel, int threads) { hipLaunchKernelGGL(kernel, dim3(total_blocks), dim3(threads), 0, s, probs, n, ext); };
+  if (dtype == DT_BF16) {
+    if (dh == 32) go(k_window_dkv_mfma<uint16_t, 32>, WinKeyCfg<uint16_t, 32>::NW * 64);
+    else if (dh == 64) go(k_window_dkv_mfma<uint16_t, 64>, WinKeyCfg<uint16_t, 64>::NW * 64);
+    else if (dh == 96) go(k_window_dkv_mfma<uint16_t, 96>, WinKeyCfg<uint16_t, 96>::NW * 64);
+    else go(k_window_dkv_mfma<uint16_t, 128>, WinKeyCfg<uint16_t, 128>::NW * 64);
+  } else {
+    if (dh == 32) go(k_window_dkv_mfma<float, 32>, WinKeyCfg<float, 32>::NW * 64);
+    else if (dh == 64) go(k_window_dkv_mfma<float, 64>, WinKeyCfg<float, 64>::NW * 64);
+    else if (dh == 96) go(k_window_dkv_mfma<float, 96>, WinKeyCfg<float, 96>::NW * 64);
+    else go(k_window_dkv_mfma<float, 128>, WinKeyCfg<float, 128>::NW * 64);
+  }
+}
+void launch_window_join(const WindowProb *probs, int n, int total_blocks, int dtype, int dh, const ExtPtrs &ext, hipStream_t s) {
+  WIN_GO(k_window_join, probs, n, ext);
+}
+
+}  // namespace gpp

@@ -148,6 +148,10 @@ struct WindowProb {
   // >= 0: entry of the per-call pointer block.  ext_out: fwd, O is written there too (entry may be null); bwd, dqkv goes there
   int32_t ext_qkv, ext_out, ext_dout, ext_len;
   int64_t ld_ext;          // fwd: row stride of the tensor behind ext_out
+  // matrix-core dK / dV: blocks of 128 keys, `whole` of them unsplit, the others cut into `parts` parts of part_steps steps, those
+  // of a sample's first tokens (sink_blocks) into sink_parts
+  GPP_G float *partial;    // fp32 sums of parts
+  int32_t sink_blocks, sink_parts, parts, part_steps, whole, units;
   int32_t blk_begin;
 };
 
@@ -359,6 +363,18 @@ void launch_window_fwd(const WindowProb *probs, int n, int total_blocks, const E
 void launch_window_dq(const WindowProb *probs, int n, int total_blocks, const ExtPtrs &ext, hipStream_t s);
 void launch_window_dkv(const WindowProb *probs, int n, int total_blocks, const ExtPtrs &ext, hipStream_t s);
 int window_max_head_dim();
+// matrix-core path: template head dimension of a record (0: none), workgroups, split of the key blocks
+int window_mfma_dh(const WindowProb &p);
+int window_mfma_query_blocks(const WindowProb &p);
+void window_plan_parts(WindowProb &p, int dh, int slots);
+int window_key_slots(int dtype, int dh);
+int window_mfma_key_blocks(const WindowProb &p);
+int window_join_blocks(const WindowProb &p, int dh);
+int64_t window_partial_bytes(const WindowProb &p, int dh);
+void launch_window_fwd_mfma(const WindowProb *probs, int n, int total_blocks, int dtype, int dh, const ExtPtrs &ext, StageFlags *flags, hipStream_t s);
+void launch_window_dq_mfma(const WindowProb *probs, int n, int total_blocks, int dtype, int dh, const ExtPtrs &ext, hipStream_t s);
+void launch_window_dkv_mfma(const WindowProb *probs, int n, int total_blocks, int dtype, int dh, const ExtPtrs &ext, hipStream_t s);
+void launch_window_join(const WindowProb *probs, int n, int total_blocks, int dtype, int dh, const ExtPtrs &ext, hipStream_t s);
 int window_blocks(int64_t batch, int heads, int seq);
 
 void launch_pool(const PoolProb *probs, int n, int total_blocks, hipStream_t s);

@@ -759,6 +759,51 @@ struct Emitter {
     return a;
   }
 
+  // one launch (backward: dQ, dK and dV, and where key blocks are split the joining of their parts) per storage type and template
+  // head dimension; 0: the row-parallel kernels
+  void emit_windows(std::vector<WindowProb> &recs, bool backward) {
+    auto mfma_dh = [&](const WindowProb &a) { return (pl.flags & 1) || (backward && a.grad_dtype != a.dtype) ? 0 : window_mfma_dh(a); };
+    auto step = [&](int kern, std::vector<WindowProb> &now, int dtype, int dh, auto blocks_of) {
+      int blocks = 0;
+      for (auto &a : now) {
+        a.blk_begin = blocks;
+        blocks += blocks_of(a);
+      }
+      if (blocks == 0) return;
+      Step &s = add_step(kern, push_table(now), (int)now.size(), blocks);
+      s.ext_kind = EXT_BOTH;
+      s.a0 = dtype;
+      s.a1 = dh;
+    };
+    for (int32_t dt : {DT_F32, DT_BF16})
+      for (int dh : {0, 32, 64, 96, 128}) {
+        std::vector<WindowProb> now;
+        for (auto &a : recs)
+          if (a.dtype == dt && mfma_dh(a) == dh) now.push_back(a);
+        if (now.empty()) continue;
+        auto queries = [&](const WindowProb &a) { return dh ? window_mfma_query_blocks(a) : window_blocks(a.batch, a.heads, a.seq); };
+        if (!backward) {
+          step(K_WINDOW_FWD, now, dt, dh, queries);
+          continue;
+        }
+        if (dh)
+          for (auto &a : now) {      // (the branches of a level share the GPU)
+            window_plan_parts(a, dh, std::max(8, window_key_slots(dt, dh) / (int)now.size() / 8 * 8));
+            const int64_t bytes = window_partial_bytes(a, dh);
+            if (bytes == 0) continue;
+            Buf b;
+            b.space = SP_SHARED;
+            b.off = pl.shared_bytes + shared_tmp_top;
+            shared_tmp_top = align_up(shared_tmp_top + bytes, 256);
+            a.partial = (float *)ptr(b);
+          }
+        step(K_WINDOW_DQ, now, dt, dh, queries);
+        step(K_WINDOW_DKV, now, dt, dh, [&](const WindowProb &a) { return dh ? window_mfma_key_blocks(a) : window_blocks(a.batch, a.kv_heads, a.seq); });
+        if (dh) step(K_WINDOW_JOIN, now, dt, dh, [&](const WindowProb &a) { return window_join_blocks(a, dh); });
+      }
+    recs.clear();
+  }
+
   // ---- elementwise helper ------------------------------------------------
   EltProb elt(const Buf &src, const Buf &dst, int64_t rows, int64_t cols) {
     EltProb e;
@@ -1606,14 +1651,7 @@ void Emitter::forward() {
       s.a1 = mfma ? 1 : 0;
     }
     emit_rotaries(rotaries);
-    if (!windows.empty()) {
-      int blocks = 0;
-      for (auto &a : windows) {
-        a.blk_begin = blocks;
-        blocks += window_blocks(a.batch, a.heads, a.seq);
-      }
-      add_step(K_WINDOW_FWD, push_table(windows), (int)windows.size(), blocks).ext_kind = EXT_BOTH;
-    }
+    emit_windows(windows, false);
     emit_elt(elts);
     if (!pools.empty()) {
       int blocks = 0;
@@ -2207,20 +2245,7 @@ void Emitter::backward() {
       s2.a0 = ms;
       s2.a1 = mfma ? 1 : 0;
     }
-    if (!windows.empty()) {
-      int blocks = 0;
-      for (auto &a : windows) {
-        a.blk_begin = blocks;
-        blocks += window_blocks(a.batch, a.heads, a.seq);
-      }
-      add_step(K_WINDOW_DQ, push_table(windows), (int)windows.size(), blocks).ext_kind = EXT_BOTH;
-      blocks = 0;
-      for (auto &a : windows) {
-        a.blk_begin = blocks;
-        blocks += window_blocks(a.batch, a.kv_heads, a.seq);
-      }
-      add_step(K_WINDOW_DKV, push_table(windows), (int)windows.size(), blocks).ext_kind = EXT_BOTH;
-    }
+    emit_windows(windows, true);
     emit_rotaries(rotaries);
     if (!pools.empty()) {
       int blocks = 0;

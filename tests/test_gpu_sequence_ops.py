@@ -113,6 +113,12 @@ def test_window_long(window, sinks):
     run_attention(b=1, seq=2500, heads=2, kv=1, dh=64, window=window, sinks=sinks, causal=False)
 
 
+@pytest.mark.parametrize("b,heads,kv,causal", [(1, 2, 1, True), (3, 4, 4, False)])
+def test_window_many_first_tokens(b, heads, kv, causal):
+    """First tokens over several blocks of keys, whose work is cut into parts, with samples that end inside them."""
+    run_attention(b=b, seq=1900, heads=heads, kv=kv, dh=64, window=100, sinks=300, causal=causal, values=[1900, 200, 700][:b])
+
+
 def test_window_forward_only():
     ops = S.attention_ops(2, 100, 4, 2, 64, window=30, sinks=2, causal=True, lengths=True, grad=False)
     batch, gout = S.draw(ops, 2, 4, lengths([55, 100]))
