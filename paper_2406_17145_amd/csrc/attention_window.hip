@@ -48,6 +48,15 @@ __global__ __launch_bounds__(256) void k_window_fwd(const WindowProb *__restrict
   const int kh = w.h / (p.heads / p.kv_heads);
   const int64_t base = (int64_t)w.b * p.seq, row = base + w.row;
   const int64_t kcol = (int64_t)(p.heads + kh) * p.dh, vcol = (int64_t)(p.heads + p.kv_heads + kh) * p.dh;
+  if (p.qkv_keep) {        // its own query, and the first of the heads that share them its key and value
+    const int blocks = w.h % (p.heads / p.kv_heads) == 0 ? 3 : 1;
+    for (int k = 0; k < blocks; ++k)
+      for (int c = lane; c < p.dh; c += 64) {
+        const int64_t col = (k == 0 ? (int64_t)w.h * p.dh : k == 1 ? kcol : vcol) + c;
+        if (p.dtype == DT_BF16) ((GPP_G uint16_t *)p.qkv_keep)[row * p.ld_keep + col] = ((const GPP_G uint16_t *)qkv)[row * p.ld_qkv + col];
+        else ((GPP_G float *)p.qkv_keep)[row * p.ld_keep + col] = ((const GPP_G float *)qkv)[row * p.ld_qkv + col];
+      }
+  }
   float o[WIN_DPL] = {0.0f}, m = -INFINITY, l = 0.0f;
   const float scale2 = p.scale * LOG2E;
   if (w.row < len) {

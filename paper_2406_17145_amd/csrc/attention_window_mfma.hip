@@ -238,10 +238,19 @@ __device__ __forceinline__ uint32_t win_tile_bytes(int rows, int64_t ld, int dh,
   return rows <= 0 ? 0u : (uint32_t)(((int64_t)(rows - 1) * ld + dh) * es);
 }
 
-// neighbouring units for the workgroups of an XCD: consecutive workgroups go round the eight XCDs
-__device__ __forceinline__ int win_spread(int idx, int total) {
+// Consecutive workgroups go round the eight XCDs, each with an L2 of its own.  Work is numbered so that `by.d` neighbours share what
+// they read (a sample's key / value head): each such run goes to one XCD, runs in turn, so that samples of unequal lengths are spread
+// over all of them; runs that are left over are cut into eight contiguous pieces.
+__device__ __forceinline__ int win_spread(int idx, int total, const FastDiv &by) {
+  const int full = divide(total >> 3, by).q * 8 * (int)by.d;
+  if (idx < full) {
+    const Quotient run = divide(idx >> 3, by);
+    return ((idx & 7) + 8 * run.q) * (int)by.d + run.r;
+  }
+  idx -= full;
+  total -= full;
   const int xcd = idx & 7, per = total >> 3, rem = total & 7;
-  return xcd * per + min(xcd, rem) + (idx >> 3);
+  return full + xcd * per + min(xcd, rem) + (idx >> 3);
 }
 
 // ---- which tiles of keys a block of queries streams -------------------------------------------------------------------
@@ -258,6 +267,18 @@ __device__ __forceinline__ WinRange win_range(const WindowProb &p, int q0, int q
   r.sinks = min((b.sink_end + KT - 1) / KT, r.first);
   r.n = r.sinks + (b.end - 1) / KT - r.first + 1;
   return r;
+}
+// a tile of K and one of V behind it, from memory to LDS byte `dst`
+template <typename T, int DH>
+__device__ __forceinline__ void win_copy_keys(const WinRange &tiles, int t, const GPP_G T *kbase, const GPP_G T *vbase, int64_t ld, int dh, int len,
+                                              int wave, const WinCopy<T, DH, 4> &co, uint32_t dst) {
+  typedef WinTile<T, DH> C;
+  const int k0 = tiles.tile(t) * C::KT;
+  const uint32_t bytes = win_tile_bytes(min(C::KT, len - k0), ld, dh, C::ES);
+  rsrc4 rk = win_rsrc(kbase + (int64_t)k0 * ld, bytes), rv = win_rsrc(vbase + (int64_t)k0 * ld, bytes);
+  settle(rk, rv);
+  win_copy(rk, co, dst, wave);
+  win_copy(rv, co, dst + C::BYTES, wave);
 }
 // what of a tile of keys a wave's queries [q0, q1] see: nothing, all of it, or some
 enum { WIN_NONE, WIN_ALL, WIN_SOME };
@@ -285,16 +306,17 @@ __device__ __forceinline__ WinWave win_wave(const WindowProb &p, int q0, int len
 // block of queries: key / value heads outermost, the query heads that share one innermost: workgroups that run together read the same
 // keys.  Where a causal block's work grows with its place, light and heavy blocks alternate, so that every XCD's share weighs the same
 struct WinBlock {
-  int b, h, r0;
+  int b, h, g, r0;       // sample, query head, key / value head, first query
+  bool first;            // of the query heads that share the key / value head
 };
-__device__ __forceinline__ WinBlock win_query_block(const WindowProb &p, int blk) {
-  const int group = p.heads / p.kv_heads, nb = (p.seq + WIN_ROWS - 1) / WIN_ROWS;
-  const int hh = blk % group, rest = blk / group, k = rest % nb, bg = rest / nb;
+__device__ __forceinline__ WinBlock win_query_block(const WindowProb &p, int blk, int rows) {
+  const Quotient hh = divide(blk, p.by_group), k = divide(hh.q, p.by_query_blocks), bg = divide(k.q, p.by_kv_heads);
   WinBlock w;
-  w.b = bg / p.kv_heads;
-  w.h = (bg % p.kv_heads) * group + hh;
-  const int qb = p.causal && !p.window ? ((k & 1) ? k >> 1 : nb - 1 - (k >> 1)) : k;
-  w.r0 = qb * WIN_ROWS;
+  w.b = bg.q;
+  w.g = bg.r;
+  w.h = bg.r * (int)p.by_group.d + hh.r;
+  w.first = hh.r == 0;
+  w.r0 = (p.causal && !p.window ? ((k.r & 1) ? k.r >> 1 : (int)p.by_query_blocks.d - 1 - (k.r >> 1)) : k.r) * rows;
   return w;
 }
 
@@ -330,82 +352,118 @@ __device__ __forceinline__ void win_store_rows(unsigned char *lds, int wave, con
   }
 }
 
-// ======================================================================= forward
+// rows [r0, r0 + rows) of a head's Q, and of K and V where it is the first of those that share them, copied for the backward pass
+template <typename T>
+__device__ __forceinline__ void win_keep(const WindowProb &p, const GPP_G T *qkv, const WinBlock &w, int64_t row0, int rows) {
+  constexpr int EPC = 16 / sizeof(T);
+  const int cpr = p.dh / EPC, n = min(rows, p.seq - w.r0), shift = cpr > 16 ? 5 : (cpr > 8 ? 4 : 3);     // threads of a row: a power of two
+  const int c = threadIdx.x & ((1 << shift) - 1);
+  if (c >= cpr) return;
+#pragma unroll
+  for (int k = 0; k < 3; ++k) {
+    if (k > 0 && !w.first) break;
+    const int64_t col = (int64_t)(k == 0 ? w.h : p.heads + (k == 1 ? 0 : p.kv_heads) + w.g) * p.dh + c * EPC;
+#pragma unroll 4
+    for (int r = threadIdx.x >> shift; r < n; r += 256 >> shift)
+      *(GPP_G u32x4 *)((GPP_G T *)p.qkv_keep + (row0 + w.r0 + r) * p.ld_keep + col) = *(const GPP_G u32x4 *)(qkv + (row0 + w.r0 + r) * p.ld_qkv + col);
+  }
+}
+
+// A wave owns 32 queries.  KG = 1: four waves, 128 queries.  KG = 2: two waves share their queries and take one half of every tile of
+// keys each, 64 queries per workgroup; for launches of so few blocks that they would leave compute units idle.
 template <typename T, int DH>
+struct WinQueryCfg {
+  typedef WinTile<T, DH> C;
+  static constexpr int NB = C::RB == 128 ? 3 : 2;                                  // buffers: as many as leave room for two workgroups' waves
+  static constexpr int CP = 2 * C::KT / C::RPG / 4;                                // copies of a wave per step
+  static constexpr int OUT = 128 * (DH * C::ES + 16), JOIN = 2 * 32 * (DH + 2) * 4;
+  static constexpr int TILES = 2 * NB * C::BYTES, LDS = TILES > OUT ? (TILES > JOIN ? TILES : JOIN) : (OUT > JOIN ? OUT : JOIN);
+};
+
+// What forward and dQ do with their tiles of K and V: a ring of NB buffers; step(t, K tile, V tile, first key)
+template <typename T, int DH, typename Step>
+__device__ __forceinline__ void win_stream_keys(const WinRange &tiles, int nt, const GPP_G T *kbase, const GPP_G T *vbase, int64_t ld, int dh, int len,
+                                                unsigned char *lds, int wave, const WinCopy<T, DH, 4> &co, uint32_t lds0, const Step &step) {
+  typedef WinTile<T, DH> C;
+  typedef WinQueryCfg<T, DH> Q;
+  int buf = Q::NB - 1 < nt ? Q::NB - 1 : 0, cur = 0;       // of the next copy, of this step
+  for (int t = 0; t < nt; ++t) {
+    if (t + Q::NB - 1 <= nt) copies_landed_barrier<(Q::NB - 2) * Q::CP>();
+    else copies_landed_barrier<0>();
+    if (t + Q::NB - 1 < nt) {
+      win_copy_keys<T, DH>(tiles, t + Q::NB - 1, kbase, vbase, ld, dh, len, wave, co, lds0 + 2 * buf * C::BYTES);
+      buf = buf + 1 == Q::NB ? 0 : buf + 1;
+    }
+    const unsigned char *tk = lds + 2 * cur * C::BYTES;
+    step(tk, tk + C::BYTES, tiles.tile(t) * C::KT);
+    cur = cur + 1 == Q::NB ? 0 : cur + 1;
+  }
+}
+
+// ======================================================================= forward
+template <typename T, int DH, int KG>
 __global__ __launch_bounds__(256, 2) void k_window_fwd_mfma(const WindowProb *__restrict__ probs, int n, ExtPtrs ext, StageFlags *flags) {
   typedef WinTile<T, DH> C;
   typedef WinFrag<T> F;
-  __shared__ __attribute__((aligned(16))) unsigned char lds[4 * C::BYTES > 128 * (DH * C::ES + 16) ? 4 * C::BYTES : 128 * (DH * C::ES + 16)];
-  const int bid = big_spread(gridDim.x);
-  const int pi = find_prob(probs, n, bid);
+  typedef WinQueryCfg<T, DH> Q;
+  constexpr int ROWS = 128 / KG;
+  __shared__ __attribute__((aligned(16))) unsigned char lds[Q::LDS];
+  const int pi = find_prob(probs, n, blockIdx.x);
   const WindowProb p = probs[pi];
-  const WinBlock w = win_query_block(p, bid - p.blk_begin);
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const WinBlock w = win_query_block(p, win_spread(blockIdx.x - p.blk_begin, p.query_units, p.by_run), ROWS);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), qg = wave & (4 / KG - 1), kg = wave / (4 / KG);
   const int len = __builtin_amdgcn_readfirstlane(window_length_checked(p, ext, w.b, w.h == 0 && w.r0 == 0 && threadIdx.x == 0, flags));
   const GPP_G T *qkv = (const GPP_G T *)(p.ext_qkv >= 0 ? ext.p[p.ext_qkv] : p.qkv);
   const int64_t row0 = (int64_t)w.b * p.seq;
-  const int kh = w.h / (p.heads / p.kv_heads);
-  const GPP_G T *kbase = qkv + row0 * p.ld_qkv + (int64_t)(p.heads + kh) * p.dh, *vbase = kbase + (int64_t)p.kv_heads * p.dh;
-  const int q0 = w.r0 + 32 * wave, q = q0 + (lane & 31), qc = max(0, min(q, len - 1));
-  const WinRange tiles = win_range<C::KT>(p, w.r0, min(w.r0 + WIN_ROWS, len) - 1, len);
+  const GPP_G T *kbase = qkv + row0 * p.ld_qkv + (int64_t)(p.heads + w.g) * p.dh, *vbase = kbase + (int64_t)p.kv_heads * p.dh;
+  const int q0 = w.r0 + 32 * qg, q = q0 + (lane & 31), qc = max(0, min(q, len - 1));
+  const WinRange tiles = win_range<C::KT>(p, w.r0, min(w.r0 + ROWS, len) - 1, len);
+  const WinCopy<T, DH, 4> co = win_copy_offsets<T, DH, 4>(wave, p.ld_qkv, p.dh);
+  const uint32_t lds0 = lds_address((const uint16_t *)lds);
+#pragma unroll
+  for (int k = 0; k < Q::NB - 1; ++k)
+    if (k < tiles.n) win_copy_keys<T, DH>(tiles, k, kbase, vbase, p.ld_qkv, p.dh, len, wave, co, lds0 + 2 * k * C::BYTES);
+  const WinRows<T, DH> qf = win_rows<T, DH>(qkv, row0 + qc, p.ld_qkv, (int64_t)w.h * p.dh, p.dh);
+  const WinLane<T, DH> at = win_lane<T, DH>();
   const WinWave mine = win_wave(p, q0, len);
   const WindowKeys keys = window_keys(p, qc, len);
   const float scale2 = p.scale * LOG2E;
-
-  const WinCopy<T, DH, 4> co = win_copy_offsets<T, DH, 4>(wave, p.ld_qkv, p.dh);
-  const uint32_t lds0 = lds_address((const uint16_t *)lds);
-  auto copy = [&](int t, int buf) {
-    const int k0 = tiles.tile(t) * C::KT;
-    const uint32_t bytes = win_tile_bytes(min(C::KT, len - k0), p.ld_qkv, p.dh, C::ES);
-    rsrc4 rk = win_rsrc(kbase + (int64_t)k0 * p.ld_qkv, bytes), rv = win_rsrc(vbase + (int64_t)k0 * p.ld_qkv, bytes);
-    settle(rk, rv);
-    win_copy(rk, co, lds0 + 2 * buf * C::BYTES, wave);
-    win_copy(rv, co, lds0 + (2 * buf + 1) * C::BYTES, wave);
-  };
-  if (tiles.n > 0) copy(0, 0);
-  const WinLane<T, DH> at = win_lane<T, DH>();
-  const WinRows<T, DH> qf = win_rows<T, DH>(qkv, row0 + qc, p.ld_qkv, (int64_t)w.h * p.dh, p.dh);
   f32x16 o[C::DB];
 #pragma unroll
   for (int d = 0; d < C::DB; ++d) o[d] = win_zero();
   float m = -INFINITY, l = 0.0f;     // running maximum (base 2, the same in a lane and its partner) and this lane's share of the sum
 
-  for (int t = 0; t < tiles.n; ++t) {
-    const int cur = t & 1;
-    copies_landed_barrier<0>();
-    if (t + 1 < tiles.n) copy(t + 1, cur ^ 1);
-    const unsigned char *tk = lds + 2 * cur * C::BYTES, *tv = tk + C::BYTES;
-    const int k0 = tiles.tile(t) * C::KT, sees = mine.sees(k0, C::KT);
-    if (sees == WIN_NONE) continue;
-    f32x16 st[C::SUB];
+  // this wave's keys of a tile, N times 32
+  auto part = [&](const unsigned char *tk, const unsigned char *tv, int k0, bool masked) {
+    constexpr int N = C::SUB / KG;
+    f32x16 st[N];
 #pragma unroll
-    for (int u = 0; u < C::SUB; ++u) {
-      st[u] = win_zero();
+    for (int i = 0; i < N; ++i) {
+      st[i] = win_zero();
 #pragma unroll
-      for (int s = 0; s < C::KS; ++s) st[u] = F::mma(win_row_frag<T, DH>(at, tk, 32 * u, s), qf.f[s], st[u]);
+      for (int s = 0; s < C::KS; ++s) st[i] = F::mma(win_row_frag<T, DH>(at, tk, 32 * i, s), qf.f[s], st[i]);
     }
-    if (sees == WIN_SOME) {
+    if (masked) {
       asm volatile("");      // keeps this a branch
       const int a = k0 - keys.first, span = keys.end - keys.first, sk = keys.sink_end - k0;
 #pragma unroll
-      for (int u = 0; u < C::SUB; ++u)
+      for (int i = 0; i < N; ++i)
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          const int j = 32 * u + win_acc_row(r);
-          if (!((unsigned)(a + j) < (unsigned)span || j < sk)) st[u][r] = -INFINITY;
+          const int j = 32 * i + win_acc_row(r);
+          if (!((unsigned)(a + j) < (unsigned)span || j < sk)) st[i][r] = -INFINITY;
         }
     }
     float mx = st[0][0];
 #pragma unroll
-    for (int u = 0; u < C::SUB; ++u)
+    for (int i = 0; i < N; ++i)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) mx = fmaxf(mx, st[u][r]);
+      for (int r = 0; r < 16; ++r) mx = fmaxf(mx, st[i][r]);
     const float m_tile = win_half_max(mx) * scale2;
     // The maximum only keeps the exponentials in range: it follows where it grew by more than 2^8, which spares most tiles the
     // rescaling of the output
     if (__ballot(m_tile > m + 8.0f) != 0ull) {
-      const float m_new = fmaxf(m, m_tile), ref = m_new == -INFINITY ? 0.0f : m_new;
-      const float alpha = __builtin_amdgcn_exp2f(m - ref);
+      const float m_new = fmaxf(m, m_tile), alpha = __builtin_amdgcn_exp2f(m - (m_new == -INFINITY ? 0.0f : m_new));
       l *= alpha;
 #pragma unroll
       for (int d = 0; d < C::DB; ++d)
@@ -415,64 +473,86 @@ __global__ __launch_bounds__(256, 2) void k_window_fwd_mfma(const WindowProb *__
     }
     const float ref = m == -INFINITY ? 0.0f : m;
 #pragma unroll
-    for (int u = 0; u < C::SUB; ++u)
+    for (int i = 0; i < N; ++i)
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        st[u][r] = __builtin_amdgcn_exp2f(fmaf(st[u][r], scale2, -ref));
-        l += st[u][r];
+        st[i][r] = __builtin_amdgcn_exp2f(fmaf(st[i][r], scale2, -ref));
+        l += st[i][r];
       }
 #pragma unroll
-    for (int c = 0; c < 2 * C::SUB; ++c) {
+    for (int c = 0; c < 2 * N; ++c) {
       const typename F::type pf = F::pack(st[c >> 1], c & 1);
 #pragma unroll
       for (int d = 0; d < C::DB; ++d) o[d] = F::mma(win_col_frag<T, DH>(at, tv, 16 * c, d), pf, o[d]);
     }
-  }
+  };
+  win_stream_keys<T, DH>(tiles, tiles.n, kbase, vbase, p.ld_qkv, p.dh, len, lds, wave, co, lds0,
+                         [&](const unsigned char *tk, const unsigned char *tv, int k0) {
+    constexpr int N = C::SUB / KG;
+    const int u = KG == 1 ? 0 : kg, sees = mine.sees(k0 + 32 * u, 32 * N);
+    if (sees != WIN_NONE) part(tk + C::at(32) * u, tv + C::at(32) * u, k0 + 32 * u, sees == WIN_SOME);
+  });
   __syncthreads();
   l = win_half_sum(l);
-  if (p.lse && lane < 32 && q < len) p.lse[((int64_t)w.b * p.heads + w.h) * p.seq + q] = m + __builtin_amdgcn_logf(l);
-  win_store_rows<T, DH>(lds, wave, o, 1.0f / l, q0, len, p.seq, p.dh, p.out, row0, p.ld_out, p.ext_out >= 0 ? (GPP_G void *)ext.p[p.ext_out] : nullptr,
-                        p.ld_ext, (int64_t)w.h * p.dh);
+  if constexpr (KG == 2) {      // the second half's output, sum and maximum to the first half's waves
+    float *join = (float *)lds + qg * 32 * (DH + 2) + lane;
+    if (kg == 1) {
+#pragma unroll
+      for (int d = 0; d < C::DB; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) join[(16 * d + r) * 64] = o[d][r];
+      if (lane < 32) {
+        join[32 * DH] = m;
+        join[32 * DH + 32] = l;
+      }
+    }
+    __syncthreads();
+    if (kg == 0) {
+      const float m1 = join[32 * DH - (lane & 32)], l1 = join[32 * DH + 32 - (lane & 32)], m_new = fmaxf(m, m1), ref = m_new == -INFINITY ? 0.0f : m_new;
+      const float a0 = __builtin_amdgcn_exp2f(m - ref), a1 = __builtin_amdgcn_exp2f(m1 - ref);
+#pragma unroll
+      for (int d = 0; d < C::DB; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[d][r] = o[d][r] * a0 + join[(16 * d + r) * 64] * a1;
+      l = l * a0 + l1 * a1;
+      m = m_new;
+    }
+    __syncthreads();
+  }
+  if (kg == 0) {
+    if (p.lse && lane < 32 && q < len) p.lse[((int64_t)w.b * p.heads + w.h) * p.seq + q] = m + __builtin_amdgcn_logf(l);
+    win_store_rows<T, DH>(lds, qg, o, 1.0f / l, q0, len, p.seq, p.dh, p.out, row0, p.ld_out, p.ext_out >= 0 ? (GPP_G void *)ext.p[p.ext_out] : nullptr,
+                          p.ld_ext, (int64_t)w.h * p.dh);
+  }
+  if (p.qkv_keep) win_keep<T>(p, qkv, w, row0, ROWS);
 }
 
 // ======================================================================= backward: dQ, and delta = rowsum(dO * O)
-template <typename T, int DH>
+template <typename T, int DH, int KG>
 __global__ __launch_bounds__(256, 2) void k_window_dq_mfma(const WindowProb *__restrict__ probs, int n, ExtPtrs ext) {
   typedef WinTile<T, DH> C;
   typedef WinFrag<T> F;
-  __shared__ __attribute__((aligned(16))) unsigned char lds[4 * C::BYTES > 128 * (DH * C::ES + 16) ? 4 * C::BYTES : 128 * (DH * C::ES + 16)];
-  const int bid = big_spread(gridDim.x);
-  const int pi = find_prob(probs, n, bid);
+  typedef WinQueryCfg<T, DH> Q;
+  constexpr int ROWS = 128 / KG;
+  __shared__ __attribute__((aligned(16))) unsigned char lds[Q::LDS];
+  const int pi = find_prob(probs, n, blockIdx.x);
   const WindowProb p = probs[pi];
-  const WinBlock w = win_query_block(p, bid - p.blk_begin);
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const WinBlock w = win_query_block(p, win_spread(blockIdx.x - p.blk_begin, p.query_units, p.by_run), ROWS);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), qg = wave & (4 / KG - 1), kg = wave / (4 / KG);
   const int len = __builtin_amdgcn_readfirstlane(window_length(p, w.b));
   const GPP_G T *qkv = (const GPP_G T *)p.qkv;
   const int64_t row0 = (int64_t)w.b * p.seq;
-  const int kh = w.h / (p.heads / p.kv_heads);
-  const GPP_G T *kbase = qkv + row0 * p.ld_qkv + (int64_t)(p.heads + kh) * p.dh, *vbase = kbase + (int64_t)p.kv_heads * p.dh;
-  const int q0 = w.r0 + 32 * wave, q = q0 + (lane & 31), qc = max(0, min(q, len - 1));
-  const WinRange tiles = win_range<C::KT>(p, w.r0, min(w.r0 + WIN_ROWS, len) - 1, len);
-  const WinWave mine = win_wave(p, q0, len);
-  WindowKeys keys = window_keys(p, qc, len);
-  if (keys.count == 1) keys.end = keys.first = keys.sink_end = 0;      // a single key's probability is constant: no gradient
-  const float scale2 = p.scale * LOG2E;
-  const int64_t stat = ((int64_t)w.b * p.heads + w.h) * p.seq + qc;
-
-  const WinCopy<T, DH, 4> co = win_copy_offsets<T, DH, 4>(wave, p.ld_qkv, p.dh);
-  const uint32_t lds0 = lds_address((const uint16_t *)lds);
-  auto copy = [&](int t, int buf) {
-    const int k0 = tiles.tile(t) * C::KT;
-    const uint32_t bytes = win_tile_bytes(min(C::KT, len - k0), p.ld_qkv, p.dh, C::ES);
-    rsrc4 rk = win_rsrc(kbase + (int64_t)k0 * p.ld_qkv, bytes), rv = win_rsrc(vbase + (int64_t)k0 * p.ld_qkv, bytes);
-    settle(rk, rv);
-    win_copy(rk, co, lds0 + 2 * buf * C::BYTES, wave);
-    win_copy(rv, co, lds0 + (2 * buf + 1) * C::BYTES, wave);
-  };
+  const GPP_G T *kbase = qkv + row0 * p.ld_qkv + (int64_t)(p.heads + w.g) * p.dh, *vbase = kbase + (int64_t)p.kv_heads * p.dh;
+  const int q0 = w.r0 + 32 * qg, q = q0 + (lane & 31), qc = max(0, min(q, len - 1));
+  const WinRange tiles = win_range<C::KT>(p, w.r0, min(w.r0 + ROWS, len) - 1, len);
   GPP_G void *dqkv = p.ext_out >= 0 ? (GPP_G void *)ext.p[p.ext_out] : p.out;
   const int nt = dqkv ? tiles.n : 0;
-  if (nt > 0) copy(0, 0);
-  const WinLane<T, DH> at = win_lane<T, DH>();
+  const WinCopy<T, DH, 4> co = win_copy_offsets<T, DH, 4>(wave, p.ld_qkv, p.dh);
+  const uint32_t lds0 = lds_address((const uint16_t *)lds);
+#pragma unroll
+  for (int k = 0; k < Q::NB - 1; ++k)
+    if (k < nt) win_copy_keys<T, DH>(tiles, k, kbase, vbase, p.ld_qkv, p.dh, len, wave, co, lds0 + 2 * k * C::BYTES);
+  const int64_t stat = ((int64_t)w.b * p.heads + w.h) * p.seq + qc;
   const WinRows<T, DH> qf = win_rows<T, DH>(qkv, row0 + qc, p.ld_qkv, (int64_t)w.h * p.dh, p.dh);
   const WinRows<T, DH> gf = win_rows<T, DH>(p.ext_dout >= 0 ? ext.p[p.ext_dout] : p.dout, row0 + qc, p.ld_dout, (int64_t)w.h * p.dh, p.dh);
   float delta = 0.0f;
@@ -483,22 +563,25 @@ __global__ __launch_bounds__(256, 2) void k_window_dq_mfma(const WindowProb *__r
 #pragma unroll
       for (int e = 0; e < 8; ++e) delta = fmaf(F::get(gf.f[s], e), F::get(of.f[s], e), delta);
     delta = win_half_sum(delta);
-    if (lane < 32 && q < len) p.delta[stat] = delta;
+    if (kg == 0 && lane < 32 && q < len) p.delta[stat] = delta;
   }
+  const WinLane<T, DH> at = win_lane<T, DH>();
+  const WinWave mine = win_wave(p, q0, len);
+  WindowKeys keys = window_keys(p, qc, len);
+  if (keys.count == 1) keys.end = keys.first = keys.sink_end = 0;      // a single key's probability is constant: no gradient
+  const float scale2 = p.scale * LOG2E;
   const float lse = q0 < len ? p.lse[stat] : 0.0f;
   f32x16 dq[C::DB];
 #pragma unroll
   for (int d = 0; d < C::DB; ++d) dq[d] = win_zero();
 
-  for (int t = 0; t < nt; ++t) {
-    const int cur = t & 1;
-    copies_landed_barrier<0>();
-    if (t + 1 < nt) copy(t + 1, cur ^ 1);
-    const unsigned char *tk = lds + 2 * cur * C::BYTES, *tv = tk + C::BYTES;
-    const int k0 = tiles.tile(t) * C::KT, sees = mine.sees(k0, C::KT);
-    if (sees == WIN_NONE) continue;
+  win_stream_keys<T, DH>(tiles, nt, kbase, vbase, p.ld_qkv, p.dh, len, lds, wave, co, lds0,
+                         [&](const unsigned char *tk, const unsigned char *tv, int k0) {
 #pragma unroll
     for (int u = 0; u < C::SUB; ++u) {
+      if (KG == 2 && u != kg) continue;
+      const int sees = mine.sees(k0 + 32 * u, 32);
+      if (sees == WIN_NONE) continue;
       f32x16 st = win_zero(), dp = win_zero();
 #pragma unroll
       for (int s = 0; s < C::KS; ++s) {
@@ -523,10 +606,28 @@ __global__ __launch_bounds__(256, 2) void k_window_dq_mfma(const WindowProb *__r
         for (int d = 0; d < C::DB; ++d) dq[d] = F::mma(win_col_frag<T, DH>(at, tk, 32 * u + 16 * c, d), sf, dq[d]);
       }
     }
-  }
+  });
   if (!dqkv) return;
   __syncthreads();
-  win_store_rows<T, DH>(lds, wave, dq, p.scale, q0, len, p.seq, p.dh, dqkv, row0, p.ld_out, nullptr, 0, (int64_t)w.h * p.dh);
+  if constexpr (KG == 2) {
+    float *join = (float *)lds + qg * 32 * (DH + 2) + lane;
+    if (kg == 1) {
+#pragma unroll
+      for (int d = 0; d < C::DB; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) join[(16 * d + r) * 64] = dq[d][r];
+    }
+    __syncthreads();
+    if (kg == 0) {
+#pragma unroll
+      for (int d = 0; d < C::DB; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) dq[d][r] += join[(16 * d + r) * 64];
+    }
+    __syncthreads();
+  }
+  if (kg == 0)
+    win_store_rows<T, DH>(lds, qg, dq, p.scale, q0, len, p.seq, p.dh, dqkv, row0, p.ld_out, nullptr, 0, (int64_t)w.h * p.dh);
 }
 
 // ======================================================================= backward: dK, dV
@@ -539,26 +640,29 @@ struct WinUnit {
   int slot;                  // of the parts of the launch
 };
 __device__ __forceinline__ WinUnit win_unit(const WindowProb &p, int idx) {
-  const int nb = (p.seq + WIN_ROWS - 1) / WIN_ROWS, nr = nb - p.sink_blocks, blocks = p.batch * p.kv_heads * nr;
+  const int rest = p.rest;     // regular blocks behind the whole ones
   WinUnit w;
   w.slot = idx - p.whole;
   w.part = -1;
-  int block, c;
-  if (idx < p.whole || w.slot < (blocks - p.whole) * p.parts) {
-    block = idx < p.whole ? idx : p.whole + w.slot / p.parts;
-    if (idx >= p.whole && p.parts > 1) w.part = w.slot % p.parts;
-    c = p.sink_blocks + block % nr;
-    block /= nr;
+  Quotient at;      // sample and head, block of keys
+  if (idx < p.whole || w.slot < rest * p.parts) {
+    Quotient k = {idx, 0};
+    if (idx >= p.whole && p.parts > 1) {
+      k = divide(w.slot, p.by_parts);
+      w.part = k.r;
+      k.q += p.whole;
+    }
+    at = divide(k.q, p.by_key_blocks);
+    at.r += p.sink_blocks;
   } else {
-    const int k = w.slot - (blocks - p.whole) * p.parts;
-    block = k / p.sink_parts;
-    if (p.sink_parts > 1) w.part = k % p.sink_parts;
-    c = block % p.sink_blocks;
-    block /= p.sink_blocks;
+    const Quotient k = divide(w.slot - rest * p.parts, p.by_sink_parts);
+    if (p.sink_parts > 1) w.part = k.r;
+    at = divide(k.q, p.by_sink_blocks);
   }
-  w.b = block / p.kv_heads;
-  w.g = block % p.kv_heads;
-  w.c0 = c * WIN_ROWS;
+  const Quotient bg = divide(at.q, p.by_kv_heads);
+  w.b = bg.q;
+  w.g = bg.r;
+  w.c0 = at.r * WIN_ROWS;
   return w;
 }
 struct WinSteps {
@@ -572,7 +676,7 @@ __device__ __forceinline__ WinSteps win_steps(const WindowProb &p, int c0, int l
     const int end = c0 < p.sinks ? len : window_queries(p, min(c0 + WIN_ROWS, len) - 1, len).end;
     w.t0 = first / KT;
     w.nt = (end - 1) / KT - w.t0 + 1;
-    w.n = w.nt * (p.heads / p.kv_heads);
+    w.n = w.nt * (int)p.by_group.d;
   }
   return w;
 }
@@ -602,9 +706,9 @@ __global__ __launch_bounds__((WinKeyCfg<T, DH>::NW * 64), (DH * sizeof(T) <= 256
   const WindowProb p = probs[pi];
   GPP_G void *dqkv = p.ext_out >= 0 ? (GPP_G void *)ext.p[p.ext_out] : p.out;
   if (!dqkv) return;
-  // (an XCD takes a run of neighbouring units: of the unsplit ones and of the others)
+  // (the unsplit units first, then the others)
   const int local = blockIdx.x - p.blk_begin;
-  const WinUnit w = win_unit(p, local < p.whole ? win_spread(local, p.whole) : p.whole + win_spread(local - p.whole, p.units - p.whole));
+  const WinUnit w = win_unit(p, local < p.whole ? win_spread(local, p.whole, p.by_key_blocks) : p.whole + win_spread(local - p.whole, p.units - p.whole, p.by_key_blocks));
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), kg = wave & 3, qg = wave >> 2;
   const int len = __builtin_amdgcn_readfirstlane(window_length(p, w.b));
   const WinSteps st_ = win_steps<C::KT>(p, w.c0, len);
@@ -615,7 +719,7 @@ __global__ __launch_bounds__((WinKeyCfg<T, DH>::NW * 64), (DH * sizeof(T) <= 256
   if (split && s0 >= s1) return;                // (such a part is not added)
   const GPP_G T *qkv = (const GPP_G T *)p.qkv, *dout = (const GPP_G T *)(p.ext_dout >= 0 ? ext.p[p.ext_dout] : p.dout);
   const int64_t row0 = (int64_t)w.b * p.seq;
-  const int group = p.heads / p.kv_heads, h0 = w.g * group;
+  const int h0 = w.g * (int)p.by_group.d;
   const int k0 = w.c0 + 32 * kg, k1 = min(k0 + 31, len - 1), kc = max(0, min(k0 + (lane & 31), len - 1));
   const int64_t kcol = (int64_t)(p.heads + w.g) * p.dh, vcol = kcol + (int64_t)p.kv_heads * p.dh;
   const WindowQueries seen = window_queries(p, kc, len);
@@ -780,7 +884,7 @@ __global__ __launch_bounds__(256) void k_window_join(const WindowProb *__restric
   const WindowProb p = probs[pi];
   GPP_G T *dqkv = (GPP_G T *)(p.ext_out >= 0 ? ext.p[p.ext_out] : p.out);
   if (!dqkv) return;
-  const int nb = (p.seq + WIN_ROWS - 1) / WIN_ROWS, rest = p.batch * p.kv_heads * (nb - p.sink_blocks) - p.whole;
+  const int rest = p.rest;
   const int regular = p.parts > 1 ? rest : 0;                     // split blocks that hold no first token
   const int blk = (blockIdx.x - p.blk_begin) / (DH / 4), piece = (blockIdx.x - p.blk_begin) % (DH / 4);
   const WinUnit w = win_unit(p, p.whole + (blk < regular ? blk * p.parts : rest * p.parts + (blk - regular) * p.sink_parts));
@@ -824,8 +928,21 @@ int window_mfma_dh(const WindowProb &p) {
   if ((p.ld_qkv | p.ld_dout) >= (1ll << 24)) return 0;        // a tile's offsets stay far inside 32 bits
   return p.dh <= 32 ? 32 : (p.dh <= 64 ? 64 : (p.dh <= 96 ? 96 : 128));
 }
-int window_mfma_query_blocks(const WindowProb &p) { return p.batch * p.heads * ((p.seq + WIN_ROWS - 1) / WIN_ROWS); }
 static int window_tile_rows(const WindowProb &p, int dh) { return dh * (p.dtype == DT_BF16 ? 2 : 4) > 256 ? 32 : 64; }
+// Two waves per 32 queries where the blocks of 128 are at most two per compute unit
+int window_key_groups(const WindowProb &p, int dh, int64_t blocks) { return window_tile_rows(p, dh) == 64 && blocks <= 512 ? 2 : 1; }
+int window_mfma_query_blocks(const WindowProb &p, int key_groups) {
+  const int rows = WIN_ROWS / key_groups;
+  return p.batch * p.heads * ((p.seq + rows - 1) / rows);
+}
+void window_plan_queries(WindowProb &p, int key_groups) {
+  const int rows = WIN_ROWS / key_groups;
+  p.by_group = fast_div(p.heads / p.kv_heads);
+  p.by_kv_heads = fast_div(p.kv_heads);
+  p.by_query_blocks = fast_div((p.seq + rows - 1) / rows);
+  p.by_run = fast_div((int64_t)p.by_group.d * p.by_query_blocks.d);
+  p.query_units = window_mfma_query_blocks(p, key_groups);
+}
 
 // Cuts the key blocks of a launch (see WinUnit) into units, of which `slots` run at once: the first `whole` blocks stay in one piece,
 // the others and the blocks of the first tokens, which take several times as long, go in parts of part_steps steps, which fill the
@@ -858,10 +975,15 @@ void window_plan_parts(WindowProb &p, int dh, int slots) {
       p.parts = (int32_t)parts;
       p.sink_parts = (int32_t)sink_parts;
       p.units = (int32_t)units;
+      p.rest = (int32_t)rest;
     }
     if (whole == 0) break;
   }
   p.sink_blocks = (int32_t)sb;
+  p.by_key_blocks = fast_div(nb - sb);
+  p.by_parts = fast_div(p.parts);
+  p.by_sink_parts = fast_div(p.sink_parts);
+  p.by_sink_blocks = fast_div(sb);
 }
 int window_mfma_key_blocks(const WindowProb &p) { return p.units; }
 int window_join_blocks(const WindowProb &p, int dh) {
@@ -874,46 +996,48 @@ int64_t window_partial_bytes(const WindowProb &p, int dh) {
 // workgroups of the dK / dV kernel that run at once: two waves per SIMD have the registers, four with heads of 32 columns in bf16
 int window_key_slots(int dtype, int dh) { return dtype == DT_BF16 && dh == 32 ? 512 : 256; }
 
-#define WIN_GO(KERNEL, ...)                                                                                       \
-  do {                                                                                                            \
-    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(total_blocks), dim3(256), 0, s, __VA_ARGS__); }; \
-    if (total_blocks <= 0) break;                                                                                 \
-    if (dtype == DT_BF16) {                                                                                       \
-      if (dh == 32) go(KERNEL<uint16_t, 32>);                                                                     \
-      else if (dh == 64) go(KERNEL<uint16_t, 64>);                                                                \
-      else if (dh == 96) go(KERNEL<uint16_t, 96>);                                                                \
-      else go(KERNEL<uint16_t, 128>);                                                                             \
-    } else {                                                                                                      \
-      if (dh == 32) go(KERNEL<float, 32>);                                                                        \
-      else if (dh == 64) go(KERNEL<float, 64>);                                                                   \
-      else if (dh == 96) go(KERNEL<float, 96>);                                                                   \
-      else go(KERNEL<float, 128>);                                                                                \
-    }                                                                                                             \
+// GO(T, DH) for a storage type and template head dimension
+#define WIN_INSTANCE(GO)                  \
+  do {                                    \
+    if (dtype == DT_BF16) {               \
+      if (dh == 32) GO(uint16_t, 32);     \
+      else if (dh == 64) GO(uint16_t, 64);\
+      else if (dh == 96) GO(uint16_t, 96);\
+      else GO(uint16_t, 128);             \
+    } else {                              \
+      if (dh == 32) GO(float, 32);        \
+      else if (dh == 64) GO(float, 64);   \
+      else if (dh == 96) GO(float, 96);   \
+      else GO(float, 128);                \
+    }                                     \
   } while (0)
+// (tiles of 32 keys are not shared: WinTile::SUB key groups at the most)
+#define WIN_QUERY_KERNEL(K, T, DH) (key_groups == 2 ? K<T, DH, WinTile<T, DH>::SUB> : K<T, DH, 1>)
 
-void launch_window_fwd_mfma(const WindowProb *probs, int n, int total_blocks, int dtype, int dh, const ExtPtrs &ext, StageFlags *flags, hipStream_t s) {
-  WIN_GO(k_window_fwd_mfma, probs, n, ext, flags);
+void launch_window_fwd_mfma(const WindowProb *probs, int n, int total_blocks, int dtype, int dh, int key_groups, const ExtPtrs &ext, StageFlags *flags,
+                            hipStream_t s) {
+  if (total_blocks <= 0) return;
+#define GO(T, DH) hipLaunchKernelGGL(WIN_QUERY_KERNEL(k_window_fwd_mfma, T, DH), dim3(total_blocks), dim3(256), 0, s, probs, n, ext, flags)
+  WIN_INSTANCE(GO);
+#undef GO
 }
-void launch_window_dq_mfma(const WindowProb *probs, int n, int total_blocks, int dtype, int dh, const ExtPtrs &ext, hipStream_t s) {
-  WIN_GO(k_window_dq_mfma, probs, n, ext);
+void launch_window_dq_mfma(const WindowProb *probs, int n, int total_blocks, int dtype, int dh, int key_groups, const ExtPtrs &ext, hipStream_t s) {
+  if (total_blocks <= 0) return;
+#define GO(T, DH) hipLaunchKernelGGL(WIN_QUERY_KERNEL(k_window_dq_mfma, T, DH), dim3(total_blocks), dim3(256), 0, s, probs, n, ext)
+  WIN_INSTANCE(GO);
+#undef GO
 }
 void launch_window_dkv_mfma(const WindowProb *probs, int n, int total_blocks, int dtype, int dh, const ExtPtrs &ext, hipStream_t s) {
   if (total_blocks <= 0) return;
-  auto go = [&](auto kernel, int threads) { hipLaunchKernelGGL(kernel, dim3(total_blocks), dim3(threads), 0, s, probs, n, ext); };
-  if (dtype == DT_BF16) {
-    if (dh == 32) go(k_window_dkv_mfma<uint16_t, 32>, WinKeyCfg<uint16_t, 32>::NW * 64);
-    else if (dh == 64) go(k_window_dkv_mfma<uint16_t, 64>, WinKeyCfg<uint16_t, 64>::NW * 64);
-    else if (dh == 96) go(k_window_dkv_mfma<uint16_t, 96>, WinKeyCfg<uint16_t, 96>::NW * 64);
-    else go(k_window_dkv_mfma<uint16_t, 128>, WinKeyCfg<uint16_t, 128>::NW * 64);
-  } else {
-    if (dh == 32) go(k_window_dkv_mfma<float, 32>, WinKeyCfg<float, 32>::NW * 64);
-    else if (dh == 64) go(k_window_dkv_mfma<float, 64>, WinKeyCfg<float, 64>::NW * 64);
-    else if (dh == 96) go(k_window_dkv_mfma<float, 96>, WinKeyCfg<float, 96>::NW * 64);
-    else go(k_window_dkv_mfma<float, 128>, WinKeyCfg<float, 128>::NW * 64);
-  }
+#define GO(T, DH) hipLaunchKernelGGL((k_window_dkv_mfma<T, DH>), dim3(total_blocks), dim3((WinKeyCfg<T, DH>::NW * 64)), 0, s, probs, n, ext)
+  WIN_INSTANCE(GO);
+#undef GO
 }
 void launch_window_join(const WindowProb *probs, int n, int total_blocks, int dtype, int dh, const ExtPtrs &ext, hipStream_t s) {
-  WIN_GO(k_window_join, probs, n, ext);
+  if (total_blocks <= 0) return;
+#define GO(T, DH) hipLaunchKernelGGL((k_window_join<T, DH>), dim3(total_blocks), dim3(256), 0, s, probs, n, ext)
+  WIN_INSTANCE(GO);
+#undef GO
 }
 
 }  // namespace gpp

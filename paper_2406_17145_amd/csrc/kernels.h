@@ -130,6 +130,13 @@ struct RotaryProb {
   int32_t rows_per_block, blk_begin;
 };
 
+// Division by a number that a launch table holds: quotients of numbers below 2^31 by a multiplication on the scalar unit (the
+// general division takes some forty instructions, and a kernel that finds its place by several of them starts a microsecond later)
+struct FastDiv {
+  uint32_t d, m;      // m = floor((2^32 - 1) / d)
+};
+inline FastDiv fast_div(int64_t d) { return {(uint32_t)(d > 0 ? d : 1), 0xffffffffu / (uint32_t)(d > 0 ? d : 1)}; }
+
 // ---- attention inside a window -----------------------------------------------
 struct WindowProb {
   const GPP_G void *qkv;   // [b*S, (heads + 2 kv_heads) dh]
@@ -140,6 +147,8 @@ struct WindowProb {
   GPP_G float *delta;      // bwd: [b*heads, S] rowsum(dO * O), written with dQ
   const GPP_G int32_t *lengths;   // [b], or null with ext_len < 0: all S
   GPP_G int32_t *lengths_keep;    // fwd, or null: the lengths are copied here for the backward pass
+  GPP_G void *qkv_keep;    // fwd, or null: the rows behind ext_qkv are copied here for the backward pass
+  int64_t ld_keep;
   int64_t ld_qkv, ld_out, ld_o, ld_dout;
   int64_t window, sinks;   // window 0: S (no limit)
   int32_t batch, heads, kv_heads, seq, dh, causal;
@@ -148,10 +157,12 @@ struct WindowProb {
   // >= 0: entry of the per-call pointer block.  ext_out: fwd, O is written there too (entry may be null); bwd, dqkv goes there
   int32_t ext_qkv, ext_out, ext_dout, ext_len;
   int64_t ld_ext;          // fwd: row stride of the tensor behind ext_out
-  // matrix-core dK / dV: blocks of 128 keys, `whole` of them unsplit, the others cut into `parts` parts of part_steps steps, those
-  // of a sample's first tokens (sink_blocks) into sink_parts
+  int32_t query_units, units;   // matrix-core kernels: workgroups of the record (forward and dQ; dK and dV)
+  // dK / dV: blocks of 128 keys, `whole` of them unsplit, the `rest` cut into `parts` parts of part_steps steps, those of a sample's
+  // first tokens (sink_blocks) into sink_parts
   GPP_G float *partial;    // fp32 sums of parts
-  int32_t sink_blocks, sink_parts, parts, part_steps, whole, units;
+  int32_t sink_blocks, sink_parts, parts, part_steps, whole, rest;
+  FastDiv by_group, by_kv_heads, by_query_blocks, by_run, by_key_blocks, by_parts, by_sink_parts, by_sink_blocks;   // matrix-core kernels
   int32_t blk_begin;
 };
 
@@ -365,14 +376,17 @@ void launch_window_dkv(const WindowProb *probs, int n, int total_blocks, const E
 int window_max_head_dim();
 // matrix-core path: template head dimension of a record (0: none), workgroups, split of the key blocks
 int window_mfma_dh(const WindowProb &p);
-int window_mfma_query_blocks(const WindowProb &p);
+// key groups of a launch of `blocks` blocks of 128 queries: how many waves share 32 queries
+int window_key_groups(const WindowProb &p, int dh, int64_t blocks);
+void window_plan_queries(WindowProb &p, int key_groups);
+int window_mfma_query_blocks(const WindowProb &p, int key_groups);
 void window_plan_parts(WindowProb &p, int dh, int slots);
 int window_key_slots(int dtype, int dh);
 int window_mfma_key_blocks(const WindowProb &p);
 int window_join_blocks(const WindowProb &p, int dh);
 int64_t window_partial_bytes(const WindowProb &p, int dh);
-void launch_window_fwd_mfma(const WindowProb *probs, int n, int total_blocks, int dtype, int dh, const ExtPtrs &ext, StageFlags *flags, hipStream_t s);
-void launch_window_dq_mfma(const WindowProb *probs, int n, int total_blocks, int dtype, int dh, const ExtPtrs &ext, hipStream_t s);
+void launch_window_fwd_mfma(const WindowProb *probs, int n, int total_blocks, int dtype, int dh, int key_groups, const ExtPtrs &ext, StageFlags *flags, hipStream_t s);
+void launch_window_dq_mfma(const WindowProb *probs, int n, int total_blocks, int dtype, int dh, int key_groups, const ExtPtrs &ext, hipStream_t s);
 void launch_window_dkv_mfma(const WindowProb *probs, int n, int total_blocks, int dtype, int dh, const ExtPtrs &ext, hipStream_t s);
 void launch_window_join(const WindowProb *probs, int n, int total_blocks, int dtype, int dh, const ExtPtrs &ext, hipStream_t s);
 int window_blocks(int64_t batch, int heads, int seq);

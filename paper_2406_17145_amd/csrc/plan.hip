@@ -275,8 +275,9 @@ gpp_status_t Plan::analyse(const gpp_stage_desc_t *desc) {
   }
 
   // ---- sequence operators on the caller's tensors ------------------------
-  // (an input that other operators read too is copied for them anyway; an attention whose input wants its gradient reads Q, K
-  // and V again in the backward pass, when the caller's tensor may be gone.  A rotary's backward pass takes its positions only)
+  // (an input that other operators read too is copied for them anyway.  An attention whose input wants its gradient reads Q, K and V
+  // again in the backward pass, when the caller's tensor may be gone: the first such reader's forward launch keeps a copy.  A
+  // rotary's backward pass takes its positions only)
   auto sequence_op = [](const Node &x) { return x.d.kind == GPP_OP_ROTARY || x.d.kind == GPP_OP_ATTENTION_WINDOW; };
   for (int i = 0; i < n; ++i) {
     Node &nd = nodes[i];
@@ -284,7 +285,7 @@ gpp_status_t Plan::analyse(const gpp_stage_desc_t *desc) {
       nd.read_direct = true;
       for (int u : nd.users) {
         const Node &c = nodes[u];
-        nd.read_direct = nd.read_direct && sequence_op(c) && !(c.d.kind == GPP_OP_ATTENTION_WINDOW && c.in[0] == i && c.wants_grad);
+        nd.read_direct = nd.read_direct && sequence_op(c);
       }
       nd.gin_direct = nd.wants_grad && nd.users.size() == 1 && sequence_op(nodes[nd.users[0]]);
     }
@@ -392,7 +393,12 @@ gpp_status_t Plan::analyse(const gpp_stage_desc_t *desc) {
     Node &nd = nodes[i];
     if (nd.val.valid() || nd.is_loss) return;
     if (nd.d.kind == GPP_OP_LINEAR && nd.fused_add >= 0) return;  // lives in the ADD's buffer
-    if (nd.read_direct && nd.d.dtype != DT_I32) return;           // (and what the backward pass does not need of an output:)
+    if (nd.read_direct && nd.d.dtype != DT_I32) {                 // (kept where an attention's backward pass reads it)
+      bool kept = false;
+      for (int u : nd.users) kept = kept || (nodes[u].d.kind == GPP_OP_ATTENTION_WINDOW && nodes[u].in[0] == i && nodes[u].wants_grad);
+      if (!kept) return;
+    }
+    // (what the backward pass does not need of an output)
     if (nd.out_direct && !(nd.d.kind == GPP_OP_ATTENTION_WINDOW && nd.wants_grad)) return;
     if (nd.val_parent >= 0) {
       alloc_val(nd.val_parent);
@@ -685,10 +691,11 @@ struct Emitter {
   }
 
   // ---- sequence operators ------------------------------------------------
-  // of the readers of an integer input that the caller's tensor is read from: the one that keeps a copy for the backward pass
+  // of the readers of an input that the caller's tensor is read from: the one that keeps a copy for the backward pass (of rows: an
+  // attention)
   bool keeps(const Node &input, int reader) const {
     for (int u : input.users)
-      if (pl.nodes[u].wants_grad) return u == reader;
+      if (pl.nodes[u].wants_grad && (input.d.dtype == DT_I32 || pl.nodes[u].d.kind == GPP_OP_ATTENTION_WINDOW)) return u == reader;
     return false;
   }
   RotaryProb rotary_record(const Node &nd, bool backward) {
@@ -763,7 +770,7 @@ struct Emitter {
   // head dimension; 0: the row-parallel kernels
   void emit_windows(std::vector<WindowProb> &recs, bool backward) {
     auto mfma_dh = [&](const WindowProb &a) { return (pl.flags & 1) || (backward && a.grad_dtype != a.dtype) ? 0 : window_mfma_dh(a); };
-    auto step = [&](int kern, std::vector<WindowProb> &now, int dtype, int dh, auto blocks_of) {
+    auto step = [&](int kern, std::vector<WindowProb> &now, int dtype, int dh, int groups, auto blocks_of) {
       int blocks = 0;
       for (auto &a : now) {
         a.blk_begin = blocks;
@@ -774,6 +781,7 @@ struct Emitter {
       s.ext_kind = EXT_BOTH;
       s.a0 = dtype;
       s.a1 = dh;
+      s.a2 = groups;
     };
     for (int32_t dt : {DT_F32, DT_BF16})
       for (int dh : {0, 32, 64, 96, 128}) {
@@ -781,9 +789,13 @@ struct Emitter {
         for (auto &a : recs)
           if (a.dtype == dt && mfma_dh(a) == dh) now.push_back(a);
         if (now.empty()) continue;
-        auto queries = [&](const WindowProb &a) { return dh ? window_mfma_query_blocks(a) : window_blocks(a.batch, a.heads, a.seq); };
+        int64_t blocks128 = 0;
+        for (auto &a : now) blocks128 += window_mfma_query_blocks(a, 1);
+        const int groups = dh ? window_key_groups(now[0], dh, blocks128) : 1;
+        for (auto &a : now) window_plan_queries(a, groups);
+        auto queries = [&](const WindowProb &a) { return dh ? window_mfma_query_blocks(a, groups) : window_blocks(a.batch, a.heads, a.seq); };
         if (!backward) {
-          step(K_WINDOW_FWD, now, dt, dh, queries);
+          step(K_WINDOW_FWD, now, dt, dh, groups, queries);
           continue;
         }
         if (dh)
@@ -797,9 +809,9 @@ struct Emitter {
             shared_tmp_top = align_up(shared_tmp_top + bytes, 256);
             a.partial = (float *)ptr(b);
           }
-        step(K_WINDOW_DQ, now, dt, dh, queries);
-        step(K_WINDOW_DKV, now, dt, dh, [&](const WindowProb &a) { return dh ? window_mfma_key_blocks(a) : window_blocks(a.batch, a.kv_heads, a.seq); });
-        if (dh) step(K_WINDOW_JOIN, now, dt, dh, [&](const WindowProb &a) { return window_join_blocks(a, dh); });
+        step(K_WINDOW_DQ, now, dt, dh, groups, queries);
+        step(K_WINDOW_DKV, now, dt, dh, 1, [&](const WindowProb &a) { return dh ? window_mfma_key_blocks(a) : window_blocks(a.batch, a.kv_heads, a.seq); });
+        if (dh) step(K_WINDOW_JOIN, now, dt, dh, 1, [&](const WindowProb &a) { return window_join_blocks(a, dh); });
       }
     recs.clear();
   }
@@ -1440,6 +1452,10 @@ void Emitter::forward() {
           if (x.read_direct) {
             a.ext_qkv = x.input_index;
             a.ld_qkv = x.feat;
+            if (keeps(x, i)) {
+              a.qkv_keep = ptr(x.val);
+              a.ld_keep = x.val.ld;
+            }
           } else {
             a.qkv = ptr(x.val);
             a.ld_qkv = x.val.ld;

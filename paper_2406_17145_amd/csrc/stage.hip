@@ -540,11 +540,11 @@ static gpp_status_t run_steps(gpp_stage *st, const std::vector<Step> &steps, int
         break;
       case K_ROTARY: launch_rotary((const RotaryProb *)tab, sp.n, sp.blocks, sp.a0, sp.a1, ext, s); break;
       case K_WINDOW_FWD:
-        if (sp.a1) launch_window_fwd_mfma((const WindowProb *)tab, sp.n, sp.blocks, sp.a0, sp.a1, ext, flags, s);
+        if (sp.a1) launch_window_fwd_mfma((const WindowProb *)tab, sp.n, sp.blocks, sp.a0, sp.a1, sp.a2, ext, flags, s);
         else launch_window_fwd((const WindowProb *)tab, sp.n, sp.blocks, ext, flags, s);
         break;
       case K_WINDOW_DQ:
-        if (sp.a1) launch_window_dq_mfma((const WindowProb *)tab, sp.n, sp.blocks, sp.a0, sp.a1, ext, s);
+        if (sp.a1) launch_window_dq_mfma((const WindowProb *)tab, sp.n, sp.blocks, sp.a0, sp.a1, sp.a2, ext, s);
         else launch_window_dq((const WindowProb *)tab, sp.n, sp.blocks, ext, s);
         break;
       case K_WINDOW_DKV:

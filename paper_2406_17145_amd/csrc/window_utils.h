@@ -6,6 +6,18 @@ namespace gpp {
 
 constexpr float LOG2E = 1.4426950408889634f;
 
+struct Quotient {
+  int q, r;
+};
+__device__ __forceinline__ Quotient divide(int n, const FastDiv &by) {
+  uint32_t q = __umulhi((uint32_t)n, by.m), r = (uint32_t)n - q * by.d;
+  if (r >= by.d) {
+    ++q;
+    r -= by.d;
+  }
+  return {(int)q, (int)r};
+}
+
 // length of sample b from the kept copy
 __device__ __forceinline__ int window_length(const WindowProb &p, int b) {
   return p.lengths ? min(max(p.lengths[b], 0), p.seq) : p.seq;

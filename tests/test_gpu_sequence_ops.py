@@ -119,6 +119,21 @@ def test_window_many_first_tokens(b, heads, kv, causal):
     run_attention(b=b, seq=1900, heads=heads, kv=kv, dh=64, window=100, sinks=300, causal=causal, values=[1900, 200, 700][:b])
 
 
+@pytest.mark.parametrize("flags", [0, 1])
+@pytest.mark.parametrize("dtype,dh", [("bf16", 64), ("f32", 24), ("bf16", 20)])
+def test_window_keeps_its_rows(dtype, dh, flags):
+    """The caller's tensor may change between the passes: the backward pass reads the stage's own copy."""
+    ops = S.attention_ops(2, 140, 6, 2, dh, window=30, sinks=2, causal=True, dtype=dtype, lengths=True)
+    batch, gout = S.draw(ops, 2, 4, lengths([140, 99]))
+    st = B.Stage(ops, 2, {}, flags=flags)
+    ins = st.stage_inputs(batch)
+    st.forward(0, ins)
+    ins[0].fill_(float("nan")), ins[1].zero_()
+    gin = st.backward(0, gout)
+    check("grad", gin[0].float().cpu().numpy(), S.oracle(ops, 2, batch, gout)[1], bars(dtype, 140)[1])
+    st.close()
+
+
 def test_window_forward_only():
     ops = S.attention_ops(2, 100, 4, 2, 64, window=30, sinks=2, causal=True, lengths=True, grad=False)
     batch, gout = S.draw(ops, 2, 4, lengths([55, 100]))
