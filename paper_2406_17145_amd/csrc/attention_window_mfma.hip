@@ -253,6 +253,25 @@ __device__ __forceinline__ int win_spread(int idx, int total, const FastDiv &by)
   return full + xcd * per + min(xcd, rem) + (idx >> 3);
 }
 
+// The fields of a record that every kernel needs, asked for in one go: read where they are used, behind branches, they come one
+// memory round trip after the other (a third of a microsecond each)
+__device__ __forceinline__ void win_fetch(const WindowProb &p) {
+  asm volatile("" ::"s"(p.qkv), "s"(p.out), "s"(p.o), "s"(p.dout), "s"(p.lse), "s"(p.delta), "s"(p.lengths), "s"(p.ld_qkv), "s"(p.ld_out), "s"(p.window),
+               "s"(p.sinks), "s"(p.heads), "s"(p.kv_heads), "s"(p.seq), "s"(p.dh), "s"(p.causal), "s"(p.scale), "s"(p.ext_out), "s"(p.query_units),
+               "s"(p.units), "s"(p.whole), "s"(p.by_group.m), "s"(p.by_kv_heads.m), "s"(p.by_key_blocks.m));
+}
+
+// Visible rows of a 32-row result as bits, shifted so that register r of the lane has bit 8 (r / 4) + r % 4; and a value kept where the
+// bit is set (two instructions an element, where comparing every row with its bounds takes five)
+__device__ __forceinline__ uint32_t win_low_bits(int n) { return (uint32_t)((1ull << min(max(n, 0), 32)) - 1); }
+__device__ __forceinline__ uint32_t win_bits(int first, int end, int sinks) {
+  return ((win_low_bits(end) & ~win_low_bits(first)) | win_low_bits(sinks)) >> (4 * ((threadIdx.x & 63) >> 5));
+}
+__device__ __forceinline__ float win_keep_bit(float v, uint32_t bits, int r, float hidden) {
+  const uint32_t t = (uint32_t)((int32_t)(bits << (31 - (8 * (r >> 2) + (r & 3)))) >> 31);
+  return __uint_as_float((__float_as_uint(v) & t) | (__float_as_uint(hidden) & ~t));
+}
+
 // ---- which tiles of keys a block of queries streams -------------------------------------------------------------------
 struct WinRange {
   int n, sinks, first;      // tiles: [0, sinks) and then [first, first + n - sinks)
@@ -268,18 +287,41 @@ __device__ __forceinline__ WinRange win_range(const WindowProb &p, int q0, int q
   r.n = r.sinks + (b.end - 1) / KT - r.first + 1;
   return r;
 }
-// a tile of K and one of V behind it, from memory to LDS byte `dst`
+// The tiles of K and V of a block of queries one after the other, each pair to LDS byte `dst`
 template <typename T, int DH>
-__device__ __forceinline__ void win_copy_keys(const WinRange &tiles, int t, const GPP_G T *kbase, const GPP_G T *vbase, int64_t ld, int dh, int len,
-                                              int wave, const WinCopy<T, DH, 4> &co, uint32_t dst) {
+struct WinKeyStream {
   typedef WinTile<T, DH> C;
-  const int k0 = tiles.tile(t) * C::KT;
-  const uint32_t bytes = win_tile_bytes(min(C::KT, len - k0), ld, dh, C::ES);
-  rsrc4 rk = win_rsrc(kbase + (int64_t)k0 * ld, bytes), rv = win_rsrc(vbase + (int64_t)k0 * ld, bytes);
-  settle(rk, rv);
-  win_copy(rk, co, dst, wave);
-  win_copy(rv, co, dst + C::BYTES, wave);
-}
+  const GPP_G T *k;             // the next tile of keys
+  int64_t ld, step, v;          // row stride; elements from tile to tile, from K to V
+  int sinks, rows;              // tiles until the jump to the window; rows of the sample from the next tile on
+  int jump;                     // rows that the jump skips
+  uint32_t whole, tail;         // bytes of a whole tile, of the sample's last one
+  __device__ __forceinline__ WinKeyStream(const GPP_G T *kbase, int64_t to_v, int64_t ld_, int dh, const WinRange &r, int len) {
+    ld = ld_;
+    v = to_v;
+    step = C::KT * ld;
+    const int first = r.sinks > 0 ? 0 : r.first * C::KT;
+    k = kbase + first * ld;
+    rows = len - first;
+    sinks = r.sinks > 0 ? r.sinks : -1;
+    jump = (r.first - r.sinks) * C::KT;
+    whole = win_tile_bytes(C::KT, ld, dh, C::ES);
+    tail = win_tile_bytes((len - 1) % C::KT + 1, ld, dh, C::ES);
+  }
+  __device__ __forceinline__ void copy(const WinCopy<T, DH, 4> &co, uint32_t dst, int wave) {
+    const uint32_t bytes = rows >= C::KT ? whole : tail;
+    rsrc4 rk = win_rsrc(k, bytes), rv = win_rsrc(k + v, bytes);
+    settle(rk, rv);
+    win_copy(rk, co, dst, wave);
+    win_copy(rv, co, dst + C::BYTES, wave);
+    k += step;
+    rows -= C::KT;
+    if (--sinks == 0) {
+      k += jump * ld;
+      rows -= jump;
+    }
+  }
+};
 // what of a tile of keys a wave's queries [q0, q1] see: nothing, all of it, or some
 enum { WIN_NONE, WIN_ALL, WIN_SOME };
 struct WinWave {
@@ -352,22 +394,31 @@ __device__ __forceinline__ void win_store_rows(unsigned char *lds, int wave, con
   }
 }
 
-// rows [r0, r0 + rows) of a head's Q, and of K and V where it is the first of those that share them, copied for the backward pass
-template <typename T>
-__device__ __forceinline__ void win_keep(const WindowProb &p, const GPP_G T *qkv, const WinBlock &w, int64_t row0, int rows) {
-  constexpr int EPC = 16 / sizeof(T);
-  const int cpr = p.dh / EPC, n = min(rows, p.seq - w.r0), shift = cpr > 16 ? 5 : (cpr > 8 ? 4 : 3);     // threads of a row: a power of two
-  const int c = threadIdx.x & ((1 << shift) - 1);
-  if (c >= cpr) return;
+// ROWS rows from w.r0 on of a head's Q, and of K and V where it is the first of those that share them, copied for the backward pass: read
+// before the results are put together and written behind them
+template <typename T, int DH, int ROWS>
+struct WinKeep {
+  static constexpr int EPC = 16 / sizeof(T), TPR = DH / EPC <= 8 ? 8 : (DH / EPC <= 16 ? 16 : 32), N = ROWS * TPR / 256;     // threads of a row, rows of a thread
+  u32x4 v[3][N];
+  template <typename Do>
+  __device__ __forceinline__ void each(const WindowProb &p, const WinBlock &w, int64_t row0, const Do &what) {
+    const int c = threadIdx.x % TPR * EPC, r = threadIdx.x / TPR;
 #pragma unroll
-  for (int k = 0; k < 3; ++k) {
-    if (k > 0 && !w.first) break;
-    const int64_t col = (int64_t)(k == 0 ? w.h : p.heads + (k == 1 ? 0 : p.kv_heads) + w.g) * p.dh + c * EPC;
-#pragma unroll 4
-    for (int r = threadIdx.x >> shift; r < n; r += 256 >> shift)
-      *(GPP_G u32x4 *)((GPP_G T *)p.qkv_keep + (row0 + w.r0 + r) * p.ld_keep + col) = *(const GPP_G u32x4 *)(qkv + (row0 + w.r0 + r) * p.ld_qkv + col);
+    for (int k = 0; k < 3; ++k) {
+      if (k > 0 && !w.first) break;
+      const int64_t col = (int64_t)(k == 0 ? w.h : p.heads + (k == 1 ? 0 : p.kv_heads) + w.g) * p.dh + c;
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        if (c < p.dh && w.r0 + r + i * (256 / TPR) < p.seq) what(v[k][i], row0 + w.r0 + r + i * (256 / TPR), col);
+    }
   }
-}
+  __device__ __forceinline__ void load(const WindowProb &p, const GPP_G T *qkv, const WinBlock &w, int64_t row0) {
+    each(p, w, row0, [&](u32x4 &x, int64_t row, int64_t col) { x = *(const GPP_G u32x4 *)(qkv + row * p.ld_qkv + col); });
+  }
+  __device__ __forceinline__ void store(const WindowProb &p, const WinBlock &w, int64_t row0) {
+    each(p, w, row0, [&](u32x4 &x, int64_t row, int64_t col) { *(GPP_G u32x4 *)((GPP_G T *)p.qkv_keep + row * p.ld_keep + col) = x; });
+  }
+};
 
 // A wave owns 32 queries.  KG = 1: four waves, 128 queries.  KG = 2: two waves share their queries and take one half of every tile of
 // keys each, 64 queries per workgroup; for launches of so few blocks that they would leave compute units idle.
@@ -380,23 +431,22 @@ struct WinQueryCfg {
   static constexpr int TILES = 2 * NB * C::BYTES, LDS = TILES > OUT ? (TILES > JOIN ? TILES : JOIN) : (OUT > JOIN ? OUT : JOIN);
 };
 
-// What forward and dQ do with their tiles of K and V: a ring of NB buffers; step(t, K tile, V tile, first key)
+// What forward and dQ do with their tiles of K and V: a ring of NB buffers; step(K tile, V tile, first key)
 template <typename T, int DH, typename Step>
-__device__ __forceinline__ void win_stream_keys(const WinRange &tiles, int nt, const GPP_G T *kbase, const GPP_G T *vbase, int64_t ld, int dh, int len,
-                                                unsigned char *lds, int wave, const WinCopy<T, DH, 4> &co, uint32_t lds0, const Step &step) {
+__device__ __forceinline__ void win_stream_keys(const WinRange &tiles, int nt, WinKeyStream<T, DH> &stream, const unsigned char *lds, int wave,
+                                                const WinCopy<T, DH, 4> &co, uint32_t lds0, const Step &step) {
   typedef WinTile<T, DH> C;
   typedef WinQueryCfg<T, DH> Q;
-  int buf = Q::NB - 1 < nt ? Q::NB - 1 : 0, cur = 0;       // of the next copy, of this step
+  uint32_t in = 2 * (Q::NB - 1) * C::BYTES, out = 0;       // buffers of the next copy and of this step
   for (int t = 0; t < nt; ++t) {
-    if (t + Q::NB - 1 <= nt) copies_landed_barrier<(Q::NB - 2) * Q::CP>();
+    if (Q::NB > 2 && t + Q::NB - 1 <= nt) copies_landed_barrier<(Q::NB - 2) * Q::CP>();
     else copies_landed_barrier<0>();
     if (t + Q::NB - 1 < nt) {
-      win_copy_keys<T, DH>(tiles, t + Q::NB - 1, kbase, vbase, ld, dh, len, wave, co, lds0 + 2 * buf * C::BYTES);
-      buf = buf + 1 == Q::NB ? 0 : buf + 1;
+      stream.copy(co, lds0 + in, wave);
+      in = in == 2 * (Q::NB - 1) * C::BYTES ? 0 : in + 2 * C::BYTES;
     }
-    const unsigned char *tk = lds + 2 * cur * C::BYTES;
-    step(tk, tk + C::BYTES, tiles.tile(t) * C::KT);
-    cur = cur + 1 == Q::NB ? 0 : cur + 1;
+    step(lds + out, lds + out + C::BYTES, tiles.tile(t) * C::KT);
+    out = out == 2 * (Q::NB - 1) * C::BYTES ? 0 : out + 2 * C::BYTES;
   }
 }
 
@@ -410,19 +460,21 @@ __global__ __launch_bounds__(256, 2) void k_window_fwd_mfma(const WindowProb *__
   __shared__ __attribute__((aligned(16))) unsigned char lds[Q::LDS];
   const int pi = find_prob(probs, n, blockIdx.x);
   const WindowProb p = probs[pi];
+  win_fetch(p);
   const WinBlock w = win_query_block(p, win_spread(blockIdx.x - p.blk_begin, p.query_units, p.by_run), ROWS);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), qg = wave & (4 / KG - 1), kg = wave / (4 / KG);
   const int len = __builtin_amdgcn_readfirstlane(window_length_checked(p, ext, w.b, w.h == 0 && w.r0 == 0 && threadIdx.x == 0, flags));
   const GPP_G T *qkv = (const GPP_G T *)(p.ext_qkv >= 0 ? ext.p[p.ext_qkv] : p.qkv);
   const int64_t row0 = (int64_t)w.b * p.seq;
-  const GPP_G T *kbase = qkv + row0 * p.ld_qkv + (int64_t)(p.heads + w.g) * p.dh, *vbase = kbase + (int64_t)p.kv_heads * p.dh;
+  const GPP_G T *kbase = qkv + row0 * p.ld_qkv + (int64_t)(p.heads + w.g) * p.dh;
   const int q0 = w.r0 + 32 * qg, q = q0 + (lane & 31), qc = max(0, min(q, len - 1));
   const WinRange tiles = win_range<C::KT>(p, w.r0, min(w.r0 + ROWS, len) - 1, len);
   const WinCopy<T, DH, 4> co = win_copy_offsets<T, DH, 4>(wave, p.ld_qkv, p.dh);
   const uint32_t lds0 = lds_address((const uint16_t *)lds);
+  WinKeyStream<T, DH> stream(kbase, (int64_t)p.kv_heads * p.dh, p.ld_qkv, p.dh, tiles, len);
 #pragma unroll
   for (int k = 0; k < Q::NB - 1; ++k)
-    if (k < tiles.n) win_copy_keys<T, DH>(tiles, k, kbase, vbase, p.ld_qkv, p.dh, len, wave, co, lds0 + 2 * k * C::BYTES);
+    if (k < tiles.n) stream.copy(co, lds0 + 2 * k * C::BYTES, wave);
   const WinRows<T, DH> qf = win_rows<T, DH>(qkv, row0 + qc, p.ld_qkv, (int64_t)w.h * p.dh, p.dh);
   const WinLane<T, DH> at = win_lane<T, DH>();
   const WinWave mine = win_wave(p, q0, len);
@@ -431,7 +483,13 @@ __global__ __launch_bounds__(256, 2) void k_window_fwd_mfma(const WindowProb *__
   f32x16 o[C::DB];
 #pragma unroll
   for (int d = 0; d < C::DB; ++d) o[d] = win_zero();
-  float m = -INFINITY, l = 0.0f;     // running maximum (base 2, the same in a lane and its partner) and this lane's share of the sum
+  float m = -INFINITY, l = 0.0f;     // running maximum (base 2, the same in a lane and its partner) and sum (in fp32 of this lane's share)
+  // Narrow heads keep the vector unit busier than the matrix cores: there the probabilities are summed as a product with a row of ones
+  constexpr bool SUM_MMA = sizeof(T) == 2 && DH <= 64;
+  f32x16 ls = win_zero();
+  typename F::type ones;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) ones[e] = (decltype(+ones[0]))1.0f;
 
   // this wave's keys of a tile, N times 32
   auto part = [&](const unsigned char *tk, const unsigned char *tv, int k0, bool masked) {
@@ -445,14 +503,13 @@ __global__ __launch_bounds__(256, 2) void k_window_fwd_mfma(const WindowProb *__
     }
     if (masked) {
       asm volatile("");      // keeps this a branch
-      const int a = k0 - keys.first, span = keys.end - keys.first, sk = keys.sink_end - k0;
 #pragma unroll
-      for (int i = 0; i < N; ++i)
+      for (int i = 0; i < N; ++i) {
+        const int j = k0 + 32 * i;
+        const uint32_t bits = win_bits(keys.first - j, keys.end - j, keys.sink_end - j);
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int j = 32 * i + win_acc_row(r);
-          if (!((unsigned)(a + j) < (unsigned)span || j < sk)) st[i][r] = -INFINITY;
-        }
+        for (int r = 0; r < 16; ++r) st[i][r] = win_keep_bit(st[i][r], bits, r, -INFINITY);
+      }
     }
     float mx = st[0][0];
 #pragma unroll
@@ -464,7 +521,8 @@ __global__ __launch_bounds__(256, 2) void k_window_fwd_mfma(const WindowProb *__
     // rescaling of the output
     if (__ballot(m_tile > m + 8.0f) != 0ull) {
       const float m_new = fmaxf(m, m_tile), alpha = __builtin_amdgcn_exp2f(m - (m_new == -INFINITY ? 0.0f : m_new));
-      l *= alpha;
+      if (SUM_MMA) ls[0] *= alpha;      // (every row of the product is the same sum: one of them is kept)
+      else l *= alpha;
 #pragma unroll
       for (int d = 0; d < C::DB; ++d)
 #pragma unroll
@@ -477,23 +535,26 @@ __global__ __launch_bounds__(256, 2) void k_window_fwd_mfma(const WindowProb *__
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         st[i][r] = __builtin_amdgcn_exp2f(fmaf(st[i][r], scale2, -ref));
-        l += st[i][r];
+        if (!SUM_MMA) l += st[i][r];
       }
 #pragma unroll
     for (int c = 0; c < 2 * N; ++c) {
       const typename F::type pf = F::pack(st[c >> 1], c & 1);
+      if (SUM_MMA) ls = F::mma(ones, pf, ls);
 #pragma unroll
       for (int d = 0; d < C::DB; ++d) o[d] = F::mma(win_col_frag<T, DH>(at, tv, 16 * c, d), pf, o[d]);
     }
   };
-  win_stream_keys<T, DH>(tiles, tiles.n, kbase, vbase, p.ld_qkv, p.dh, len, lds, wave, co, lds0,
+  win_stream_keys<T, DH>(tiles, tiles.n, stream, lds, wave, co, lds0,
                          [&](const unsigned char *tk, const unsigned char *tv, int k0) {
     constexpr int N = C::SUB / KG;
     const int u = KG == 1 ? 0 : kg, sees = mine.sees(k0 + 32 * u, 32 * N);
     if (sees != WIN_NONE) part(tk + C::at(32) * u, tv + C::at(32) * u, k0 + 32 * u, sees == WIN_SOME);
   });
+  WinKeep<T, DH, ROWS> keep;
+  if (p.qkv_keep) keep.load(p, qkv, w, row0);
   __syncthreads();
-  l = win_half_sum(l);
+  l = SUM_MMA ? ls[0] : win_half_sum(l);
   if constexpr (KG == 2) {      // the second half's output, sum and maximum to the first half's waves
     float *join = (float *)lds + qg * 32 * (DH + 2) + lane;
     if (kg == 1) {
@@ -524,7 +585,7 @@ __global__ __launch_bounds__(256, 2) void k_window_fwd_mfma(const WindowProb *__
     win_store_rows<T, DH>(lds, qg, o, 1.0f / l, q0, len, p.seq, p.dh, p.out, row0, p.ld_out, p.ext_out >= 0 ? (GPP_G void *)ext.p[p.ext_out] : nullptr,
                           p.ld_ext, (int64_t)w.h * p.dh);
   }
-  if (p.qkv_keep) win_keep<T>(p, qkv, w, row0, ROWS);
+  if (p.qkv_keep) keep.store(p, w, row0);
 }
 
 // ======================================================================= backward: dQ, and delta = rowsum(dO * O)
@@ -537,21 +598,23 @@ __global__ __launch_bounds__(256, 2) void k_window_dq_mfma(const WindowProb *__r
   __shared__ __attribute__((aligned(16))) unsigned char lds[Q::LDS];
   const int pi = find_prob(probs, n, blockIdx.x);
   const WindowProb p = probs[pi];
+  win_fetch(p);
   const WinBlock w = win_query_block(p, win_spread(blockIdx.x - p.blk_begin, p.query_units, p.by_run), ROWS);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), qg = wave & (4 / KG - 1), kg = wave / (4 / KG);
   const int len = __builtin_amdgcn_readfirstlane(window_length(p, w.b));
   const GPP_G T *qkv = (const GPP_G T *)p.qkv;
   const int64_t row0 = (int64_t)w.b * p.seq;
-  const GPP_G T *kbase = qkv + row0 * p.ld_qkv + (int64_t)(p.heads + w.g) * p.dh, *vbase = kbase + (int64_t)p.kv_heads * p.dh;
+  const GPP_G T *kbase = qkv + row0 * p.ld_qkv + (int64_t)(p.heads + w.g) * p.dh;
   const int q0 = w.r0 + 32 * qg, q = q0 + (lane & 31), qc = max(0, min(q, len - 1));
   const WinRange tiles = win_range<C::KT>(p, w.r0, min(w.r0 + ROWS, len) - 1, len);
   GPP_G void *dqkv = p.ext_out >= 0 ? (GPP_G void *)ext.p[p.ext_out] : p.out;
   const int nt = dqkv ? tiles.n : 0;
   const WinCopy<T, DH, 4> co = win_copy_offsets<T, DH, 4>(wave, p.ld_qkv, p.dh);
   const uint32_t lds0 = lds_address((const uint16_t *)lds);
+  WinKeyStream<T, DH> stream(kbase, (int64_t)p.kv_heads * p.dh, p.ld_qkv, p.dh, tiles, len);
 #pragma unroll
   for (int k = 0; k < Q::NB - 1; ++k)
-    if (k < nt) win_copy_keys<T, DH>(tiles, k, kbase, vbase, p.ld_qkv, p.dh, len, wave, co, lds0 + 2 * k * C::BYTES);
+    if (k < nt) stream.copy(co, lds0 + 2 * k * C::BYTES, wave);
   const int64_t stat = ((int64_t)w.b * p.heads + w.h) * p.seq + qc;
   const WinRows<T, DH> qf = win_rows<T, DH>(qkv, row0 + qc, p.ld_qkv, (int64_t)w.h * p.dh, p.dh);
   const WinRows<T, DH> gf = win_rows<T, DH>(p.ext_dout >= 0 ? ext.p[p.ext_dout] : p.dout, row0 + qc, p.ld_dout, (int64_t)w.h * p.dh, p.dh);
@@ -563,7 +626,7 @@ __global__ __launch_bounds__(256, 2) void k_window_dq_mfma(const WindowProb *__r
 #pragma unroll
       for (int e = 0; e < 8; ++e) delta = fmaf(F::get(gf.f[s], e), F::get(of.f[s], e), delta);
     delta = win_half_sum(delta);
-    if (kg == 0 && lane < 32 && q < len) p.delta[stat] = delta;
+    if (kg == 0 && lane < 32 && q < len) p.delta[stat] = -delta;      // (as the dK / dV kernel takes it)
   }
   const WinLane<T, DH> at = win_lane<T, DH>();
   const WinWave mine = win_wave(p, q0, len);
@@ -575,7 +638,7 @@ __global__ __launch_bounds__(256, 2) void k_window_dq_mfma(const WindowProb *__r
 #pragma unroll
   for (int d = 0; d < C::DB; ++d) dq[d] = win_zero();
 
-  win_stream_keys<T, DH>(tiles, nt, kbase, vbase, p.ld_qkv, p.dh, len, lds, wave, co, lds0,
+  win_stream_keys<T, DH>(tiles, nt, stream, lds, wave, co, lds0,
                          [&](const unsigned char *tk, const unsigned char *tv, int k0) {
 #pragma unroll
     for (int u = 0; u < C::SUB; ++u) {
@@ -592,12 +655,10 @@ __global__ __launch_bounds__(256, 2) void k_window_dq_mfma(const WindowProb *__r
       for (int r = 0; r < 16; ++r) st[r] = __builtin_amdgcn_exp2f(fmaf(st[r], scale2, -lse)) * (dp[r] - delta);
       if (sees == WIN_SOME) {
         asm volatile("");
-        const int a = k0 - keys.first, span = keys.end - keys.first, sk = keys.sink_end - k0;
+        const int j = k0 + 32 * u;
+        const uint32_t bits = win_bits(keys.first - j, keys.end - j, keys.sink_end - j);
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int j = 32 * u + win_acc_row(r);
-          if (!((unsigned)(a + j) < (unsigned)span || j < sk)) st[r] = 0.0f;
-        }
+        for (int r = 0; r < 16; ++r) st[r] = win_keep_bit(st[r], bits, r, 0.0f);
       }
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
@@ -692,7 +753,9 @@ struct WinKeyCfg {
   static constexpr bool V_LDS = sizeof(T) == 2 && DH > 64;
   static constexpr int V_BYTES = V_LDS ? WIN_ROWS / C::RPG * C::GROUP : 0, ST = DH * C::ES + 16;
   static constexpr int JOIN = QG > 1 ? 4 * 32 * DH * 4 : 0, OUT = 4 * 32 * ST;    // over the tiles: a sum of four waves, rows of the result
-  static constexpr int TILES = 2 * BUF + V_BYTES, LDS = TILES > JOIN ? (TILES > OUT ? TILES : OUT) : (JOIN > OUT ? JOIN : OUT);
+  static constexpr int NB = C::RB == 128 ? 4 : (DH * C::ES > 256 ? 2 : 3);         // buffers, as many as the LDS of a compute unit's workgroups holds
+  static constexpr int CP = 2 * C::KT / C::RPG / NW;                               // copies of a wave per step, at least
+  static constexpr int TILES = NB * BUF + V_BYTES, LDS = TILES > JOIN ? (TILES > OUT ? TILES : OUT) : (JOIN > OUT ? JOIN : OUT);
 };
 
 template <typename T, int DH>
@@ -704,6 +767,7 @@ __global__ __launch_bounds__((WinKeyCfg<T, DH>::NW * 64), (DH * sizeof(T) <= 256
   __shared__ __attribute__((aligned(16))) unsigned char lds[K::LDS];
   const int pi = find_prob(probs, n, blockIdx.x);
   const WindowProb p = probs[pi];
+  win_fetch(p);
   GPP_G void *dqkv = p.ext_out >= 0 ? (GPP_G void *)ext.p[p.ext_out] : p.out;
   if (!dqkv) return;
   // (the unsplit units first, then the others)
@@ -727,42 +791,60 @@ __global__ __launch_bounds__((WinKeyCfg<T, DH>::NW * 64), (DH * sizeof(T) <= 256
   // queries that see one key only have no gradient of their score: all of them, or the first
   const bool all_single = (win == 1 && nsink == 0) || len == 1, first_single = p.causal || (win == 1 && min(nsink, len) <= 1);
   const float scale2 = p.scale * LOG2E;
+  // queries that see one of this wave's keys, and those that see all of them
+  const int kl = max(0, k1);
+  const int any_first = window_queries(p, min(k0, kl), len).first, any_end = k0 < len ? (k0 < nsink ? len : window_queries(p, kl, len).end) : 0;
+  const int all_first = window_queries(p, kl, len).first, all_end = window_queries(p, k0 < nsink && nsink <= kl ? nsink : min(k0, kl), len).end;
 
   const WinCopy<T, DH, K::NW> cq = win_copy_offsets<T, DH, K::NW>(wave, p.ld_qkv, p.dh), cg = win_copy_offsets<T, DH, K::NW>(wave, p.ld_dout, p.dh);
   const uint32_t lds0 = lds_address((const uint16_t *)lds);
-  int head = s0 < s1 ? s0 / nt : 0, tile = s0 - head * nt;      // of the next step to be copied
+  // of the next step to be copied: tile of its head, rows of the sample from there on, Q, dO, and (wave 0, 1) log-sum-exps or deltas
+  int head = s0 < s1 ? s0 / nt : 0, tile = s0 - head * nt, rows = len - (t0 + tile) * C::KT;
+  const GPP_G T *qn = qkv + (row0 + (t0 + tile) * C::KT) * p.ld_qkv + (int64_t)(h0 + head) * p.dh;
+  const GPP_G T *gn = dout + (row0 + (t0 + tile) * C::KT) * p.ld_dout + (int64_t)(h0 + head) * p.dh;
+  const GPP_G float *sn = (wave == 0 ? p.lse : p.delta) + ((int64_t)w.b * p.heads + h0 + head) * p.seq + (t0 + tile) * C::KT;
+  const int64_t q_step = C::KT * p.ld_qkv, g_step = C::KT * p.ld_dout;
+  const uint32_t q_whole = win_tile_bytes(C::KT, p.ld_qkv, p.dh, C::ES), q_tail = win_tile_bytes((len - 1) % C::KT + 1, p.ld_qkv, p.dh, C::ES);
+  const uint32_t g_whole = win_tile_bytes(C::KT, p.ld_dout, p.dh, C::ES), g_tail = win_tile_bytes((len - 1) % C::KT + 1, p.ld_dout, p.dh, C::ES);
   auto copy_next = [&](int buf) {
-    const int h = h0 + head, i0 = (t0 + tile) * C::KT, rows = min(C::KT, len - i0);
-    rsrc4 rq = win_rsrc(qkv + (row0 + i0) * p.ld_qkv + (int64_t)h * p.dh, win_tile_bytes(rows, p.ld_qkv, p.dh, C::ES));
-    rsrc4 rg = win_rsrc(dout + (row0 + i0) * p.ld_dout + (int64_t)h * p.dh, win_tile_bytes(rows, p.ld_dout, p.dh, C::ES));
+    const bool full = rows >= C::KT;
+    rsrc4 rq = win_rsrc(qn, full ? q_whole : q_tail), rg = win_rsrc(gn, full ? g_whole : g_tail);
     settle(rq, rg);
     win_copy(rq, cq, lds0 + buf * K::BUF, wave);
     win_copy(rg, cg, lds0 + buf * K::BUF + C::BYTES, wave);
-    if (wave < 2) {      // one wave the log-sum-exps, one the deltas (queries behind the end: zero, as their rows)
-      const int64_t stat = ((int64_t)w.b * p.heads + h) * p.seq + i0;
-      rsrc4 rs = win_rsrc((wave ? p.delta : p.lse) + stat, (uint32_t)max(rows, 0) * 4), same = rs;
+    if (wave < 2) {      // (queries behind the end: zero, as their rows)
+      rsrc4 rs = win_rsrc(sn, (uint32_t)min(rows, C::KT) * 4), same = rs;
       settle(rs, same);
       lds_copy4(rs, lds0 + buf * K::BUF + 2 * C::BYTES + wave * 512, lane * 4);
     }
-    if (++tile == nt) {
+    qn += q_step;
+    gn += g_step;
+    sn += C::KT;
+    rows -= C::KT;
+    if (++tile == nt) {      // the next head's first tile
       tile = 0;
-      ++head;
+      qn += p.dh - nt * q_step;
+      gn += p.dh - nt * g_step;
+      sn += p.seq - nt * C::KT;
+      rows += nt * C::KT;
     }
   };
   int now = tile;       // of the step that is being multiplied
-  if (s0 < s1) {
-    copy_next(0);
-    if constexpr (K::V_LDS) {      // 128 rows of V: two tiles' worth
+  if constexpr (K::V_LDS) {
+    if (s0 < s1) {      // 128 rows of V: two tiles' worth
       const WinCopy<T, DH, K::NW> cv = win_copy_offsets<T, DH, K::NW>(wave, p.ld_qkv, p.dh);
 #pragma unroll
       for (int half = 0; half < WIN_ROWS / C::KT; ++half) {
         const int r0 = w.c0 + half * C::KT;
         rsrc4 rv = win_rsrc(qkv + (row0 + min(r0, len - 1)) * p.ld_qkv + vcol, win_tile_bytes(min(C::KT, len - r0), p.ld_qkv, p.dh, C::ES)), same = rv;
         settle(rv, same);
-        win_copy(rv, cv, lds0 + 2 * K::BUF + half * C::BYTES, wave);
+        win_copy(rv, cv, lds0 + K::NB * K::BUF + half * C::BYTES, wave);
       }
     }
   }
+#pragma unroll
+  for (int k = 0; k < K::NB - 1; ++k)
+    if (s0 + k < s1) copy_next(k);
   const WinLane<T, DH> at = win_lane<T, DH>();
   const WinRows<T, DH> kf = win_rows<T, DH>(qkv, row0 + kc, p.ld_qkv, kcol, p.dh);
   WinRows<T, DH> vf;
@@ -771,39 +853,52 @@ __global__ __launch_bounds__((WinKeyCfg<T, DH>::NW * 64), (DH * sizeof(T) <= 256
 #pragma unroll
   for (int d = 0; d < C::DB; ++d) dk[d] = dv[d] = win_zero();
 
+  int in = K::NB - 1, out = 0;       // buffers of the next copy and of this step
   for (int s = s0; s < s1; ++s) {
-    const int cur = (s - s0) & 1;
-    copies_landed_barrier<0>();
-    if (s + 1 < s1) copy_next(cur ^ 1);
-    const unsigned char *tq = lds + cur * K::BUF, *tg = tq + C::BYTES;
-    const int i0 = (t0 + now) * C::KT + 32 * qg, i1 = min(i0 + 31, len - 1);
+    if (s + K::NB - 1 <= s1) copies_landed_barrier<(K::NB - 2) * K::CP>();
+    else copies_landed_barrier<0>();
+    if (s + K::NB - 1 < s1) {
+      copy_next(in);
+      in = in + 1 == K::NB ? 0 : in + 1;
+    }
+    const unsigned char *tq = lds + out * K::BUF, *tg = tq + C::BYTES;
+    out = out + 1 == K::NB ? 0 : out + 1;
+    const int i0 = (t0 + now) * C::KT + 32 * qg;
     now = now + 1 == nt ? 0 : now + 1;
-    if (k0 >= len || i0 >= len || (p.causal && i1 < k0) || !(k0 < nsink || (i0 - k1 < win && k0 - i1 < win))) continue;
-    const bool all = (!p.causal || k1 <= i0) && (k1 < nsink || (i1 - k0 < win && k1 - i0 < win));
+    if (i0 >= any_end || i0 + 32 <= any_first) continue;
+    const bool all = i0 >= all_first && min(i0 + 32, len) <= all_end;
     const float *tl = (const float *)(tq + 2 * C::BYTES) + 32 * qg + 4 * (lane >> 5), *td = tl + 128;
-    f32x16 st = win_zero(), dp = win_zero();
+    f32x16 st = win_zero(), dp;      // (dP - delta: the products are added to -delta)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const f32x4 minus = *(const f32x4 *)(td + 8 * k);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) dp[4 * k + e] = minus[e];
+    }
 #pragma unroll
     for (int x = 0; x < C::KS; ++x) {
       st = F::mma(win_row_frag<T, DH>(at, tq + C::at(32) * qg, 0, x), kf.f[x], st);
-      if constexpr (K::V_LDS) dp = F::mma(win_row_frag<T, DH>(at, tg + C::at(32) * qg, 0, x), win_row_frag<T, DH>(at, lds + 2 * K::BUF + C::at(32) * kg, 0, x), dp);
+      if constexpr (K::V_LDS) dp = F::mma(win_row_frag<T, DH>(at, tg + C::at(32) * qg, 0, x), win_row_frag<T, DH>(at, lds + K::NB * K::BUF + C::at(32) * kg, 0, x), dp);
       else dp = F::mma(win_row_frag<T, DH>(at, tg + C::at(32) * qg, 0, x), vf.f[x], dp);
     }
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      const f32x4 lse = *(const f32x4 *)(tl + 8 * k), delta = *(const f32x4 *)(td + 8 * k);
+      const f32x4 lse = *(const f32x4 *)(tl + 8 * k);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const int r = 4 * k + e;
         st[r] = __builtin_amdgcn_exp2f(fmaf(st[r], scale2, -lse[e]));
-        dp[r] = st[r] * (dp[r] - delta[e]);
+        dp[r] *= st[r];
       }
     }
     if (!all) {
       asm volatile("");      // keeps this a branch
-      const int a = i0 - seen.first, span = seen.end - seen.first;
+      const uint32_t bits = win_bits(seen.first - i0, seen.end - i0, 0);
 #pragma unroll
-      for (int r = 0; r < 16; ++r)
-        if (!((unsigned)(a + win_acc_row(r)) < (unsigned)span)) st[r] = dp[r] = 0.0f;
+      for (int r = 0; r < 16; ++r) {
+        st[r] = win_keep_bit(st[r], bits, r, 0.0f);
+        dp[r] = win_keep_bit(dp[r], bits, r, 0.0f);
+      }
       if (i0 == 0 && first_single && lane < 32) dp[0] = 0.0f;
     }
 #pragma unroll
@@ -947,8 +1042,9 @@ void window_plan_queries(WindowProb &p, int key_groups) {
 // Cuts the key blocks of a launch (see WinUnit) into units, of which `slots` run at once: the first `whole` blocks stay in one piece,
 // the others and the blocks of the first tokens, which take several times as long, go in parts of part_steps steps, which fill the
 // gaps that whole blocks leave.  Of the pairs (whole, part_steps) the one with the least estimate, in steps: what a slot has to do, but
-// no less than the rounds of whole blocks, plus half a part of unevenness; a unit costs four steps for its operands and its
-// result, a part its sums' way through memory, the joining launch a few steps.
+// no less than the rounds of whole blocks, plus half a part of unevenness; a unit costs the time of some steps for its operands
+// and its result (4 us: about four steps of 64 x 128 pairs in bf16, half a one in fp32), a part its sums' way through memory, the
+// joining launch (5 us) the same for all.
 void window_plan_parts(WindowProb &p, int dh, int slots) {
   const int64_t kt = window_tile_rows(p, dh), group = p.heads / p.kv_heads, seq = p.seq, nb = (seq + WIN_ROWS - 1) / WIN_ROWS;
   const int64_t win = p.window ? std::min<int64_t>(p.window, seq) : seq, bg = (int64_t)p.batch * p.kv_heads;
@@ -957,17 +1053,18 @@ void window_plan_parts(WindowProb &p, int dh, int slots) {
   const int64_t regular = group * tiles(WIN_ROWS - 1 + (p.causal ? win : 2 * win - 1)), every = group * tiles(seq), blocks = bg * (nb - sb);
   const bool triangle = p.causal && !p.window;       // half of the steps of a regular block, on average; the first blocks have most
   auto up = [](int64_t v, int64_t by) { return (v + by - 1) / by; };
+  const double start = p.dtype == DT_BF16 ? 4.0 : 0.5, join = p.dtype == DT_BF16 ? 6.0 : 0.75, sums = p.dtype == DT_BF16 ? 0.00035 * dh : 0.00005 * dh;
   double best = 1e300;
   for (int64_t whole = blocks;; whole = std::max<int64_t>(0, std::min(whole - 1, whole - slots / 8) / 8 * 8)) {
-    for (int64_t part = 8; part < 2 * every + 8; part += part < 32 ? 4 : part / 8) {
+    for (int64_t part = p.dtype == DT_BF16 ? 8 : 1; part < 2 * every + 8; part += part < 8 ? 1 : (part < 32 ? 4 : part / 8)) {
       const int64_t rest = blocks - whole, parts = up(regular, part), sink_parts = sb ? up(every, part) : 1;
       const int64_t split = (parts > 1 ? rest * parts : 0) + (sink_parts > 1 ? bg * sb * sink_parts : 0);
       const int64_t units = whole + rest * parts + bg * sb * sink_parts;
       const double steps = (double)blocks * regular * (triangle ? 0.5 : 1.0) + (double)(bg * sb * every);
-      const double slot = (steps + 4.0 * (double)units) / slots;
-      const double longest = std::max((double)(whole ? regular : 0), (double)std::min(part, std::max(rest ? regular : 0, sb ? every : 0))) + 4.0;
-      const double rounds = triangle ? longest : (double)up(whole, slots) * (regular + 4.0);
-      const double t = std::max(std::max(slot, longest), rounds) + 0.5 * (split ? (double)part : 0.0) + (split ? 6.0 + 0.00035 * dh * (double)split : 0.0);
+      const double slot = (steps + start * (double)units) / slots;
+      const double longest = std::max((double)(whole ? regular : 0), (double)std::min(part, std::max(rest ? regular : 0, sb ? every : 0))) + start;
+      const double rounds = triangle ? longest : (double)up(whole, slots) * (regular + start);
+      const double t = std::max(std::max(slot, longest), rounds) + 0.5 * (split ? (double)part : 0.0) + (split ? join + sums * (double)split : 0.0);
       if (t >= best) continue;
       best = t;
       p.whole = (int32_t)whole;
