@@ -752,7 +752,7 @@ struct WinKeyCfg {
   static constexpr int QG = C::SUB, NW = 4 * QG, BUF = 2 * C::BYTES + 1024;      // Q, dO, and the log-sum-exps and deltas of the tile's queries
   static constexpr bool V_LDS = sizeof(T) == 2 && DH > 64;
   static constexpr int V_BYTES = V_LDS ? WIN_ROWS / C::RPG * C::GROUP : 0, ST = DH * C::ES + 16;
-  static constexpr int JOIN = QG > 1 ? 4 * 32 * DH * 4 : 0, OUT = 4 * 32 * ST;    // over the tiles: a sum of four waves, rows of the result
+  static constexpr int JOIN = QG > 1 ? NW * 32 * DH * 4 : 0, OUT = NW * 32 * ST;    // over the tiles: a half of every wave's sums, rows of the result
   static constexpr int NB = C::RB == 128 ? 4 : (DH * C::ES > 256 ? 2 : 3);         // buffers, as many as the LDS of a compute unit's workgroups holds
   static constexpr int CP = 2 * C::KT / C::RPG / NW;                               // copies of a wave per step, at least
   static constexpr int TILES = NB * BUF + V_BYTES, LDS = TILES > JOIN ? (TILES > OUT ? TILES : OUT) : (JOIN > OUT ? JOIN : OUT);
@@ -786,16 +786,6 @@ __global__ __launch_bounds__((WinKeyCfg<T, DH>::NW * 64), (DH * sizeof(T) <= 256
   const int h0 = w.g * (int)p.by_group.d;
   const int k0 = w.c0 + 32 * kg, k1 = min(k0 + 31, len - 1), kc = max(0, min(k0 + (lane & 31), len - 1));
   const int64_t kcol = (int64_t)(p.heads + w.g) * p.dh, vcol = kcol + (int64_t)p.kv_heads * p.dh;
-  const WindowQueries seen = window_queries(p, kc, len);
-  const int win = (int)min(p.window ? p.window : (int64_t)p.seq, (int64_t)p.seq), nsink = (int)min(p.sinks, (int64_t)p.seq);
-  // queries that see one key only have no gradient of their score: all of them, or the first
-  const bool all_single = (win == 1 && nsink == 0) || len == 1, first_single = p.causal || (win == 1 && min(nsink, len) <= 1);
-  const float scale2 = p.scale * LOG2E;
-  // queries that see one of this wave's keys, and those that see all of them
-  const int kl = max(0, k1);
-  const int any_first = window_queries(p, min(k0, kl), len).first, any_end = k0 < len ? (k0 < nsink ? len : window_queries(p, kl, len).end) : 0;
-  const int all_first = window_queries(p, kl, len).first, all_end = window_queries(p, k0 < nsink && nsink <= kl ? nsink : min(k0, kl), len).end;
-
   const WinCopy<T, DH, K::NW> cq = win_copy_offsets<T, DH, K::NW>(wave, p.ld_qkv, p.dh), cg = win_copy_offsets<T, DH, K::NW>(wave, p.ld_dout, p.dh);
   const uint32_t lds0 = lds_address((const uint16_t *)lds);
   // of the next step to be copied: tile of its head, rows of the sample from there on, Q, dO, and (wave 0, 1) log-sum-exps or deltas
@@ -845,6 +835,15 @@ __global__ __launch_bounds__((WinKeyCfg<T, DH>::NW * 64), (DH * sizeof(T) <= 256
 #pragma unroll
   for (int k = 0; k < K::NB - 1; ++k)
     if (s0 + k < s1) copy_next(k);
+  const WindowQueries seen = window_queries(p, kc, len);
+  const int win = (int)min(p.window ? p.window : (int64_t)p.seq, (int64_t)p.seq), nsink = (int)min(p.sinks, (int64_t)p.seq);
+  // queries that see one key only have no gradient of their score: all of them, or the first
+  const bool all_single = (win == 1 && nsink == 0) || len == 1, first_single = p.causal || (win == 1 && min(nsink, len) <= 1);
+  const float scale2 = p.scale * LOG2E;
+  // queries that see one of this wave's keys, and those that see all of them
+  const int kl = max(0, k1);
+  const int any_first = window_queries(p, min(k0, kl), len).first, any_end = k0 < len ? (k0 < nsink ? len : window_queries(p, kl, len).end) : 0;
+  const int all_first = window_queries(p, kl, len).first, all_end = window_queries(p, k0 < nsink && nsink <= kl ? nsink : min(k0, kl), len).end;
   const WinLane<T, DH> at = win_lane<T, DH>();
   const WinRows<T, DH> kf = win_rows<T, DH>(qkv, row0 + kc, p.ld_qkv, kcol, p.dh);
   WinRows<T, DH> vf;
@@ -912,60 +911,52 @@ __global__ __launch_bounds__((WinKeyCfg<T, DH>::NW * 64), (DH * sizeof(T) <= 256
     }
   }
   __syncthreads();
-  if constexpr (K::QG > 1) {      // the second half's sums to the first half's waves, dK and then dV
-    float *sums = (float *)lds + kg * 32 * DH + lane;
-#pragma unroll
-    for (int which = 0; which < 2; ++which) {
-      f32x16(&acc)[C::DB] = which ? dv : dk;
-      if (qg == 1) {
-#pragma unroll
-        for (int d = 0; d < C::DB; ++d)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) sums[(d * 16 + r) * 64] = acc[d][r];
-      }
-      __syncthreads();
-      if (qg == 0) {
-#pragma unroll
-        for (int d = 0; d < C::DB; ++d)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) acc[d][r] += sums[(d * 16 + r) * 64];
-      }
-      __syncthreads();
-    }
-    if (qg == 1) return;
-  }
-  const float mk = all_single ? 0.0f : p.scale;
-  if (split) {     // [part of the launch][dK, dV][key][column] in fp32
-    GPP_G float *part = p.partial + (int64_t)w.slot * 2 * WIN_ROWS * DH + (int64_t)(32 * kg) * DH + (lane & 31);
+  // the waves that share keys give each other a half of the sums: the first takes dK, the second dV
+  if constexpr (K::QG > 1) {
+    float *sums = (float *)lds + kg * 32 * DH + lane, *theirs = sums + (1 - qg) * 4 * 32 * DH;
+    sums += qg * 4 * 32 * DH;
 #pragma unroll
     for (int d = 0; d < C::DB; ++d)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        part[win_acc_row(r) * DH + 32 * d] = dk[d][r] * mk;
-        part[(WIN_ROWS + win_acc_row(r)) * DH + 32 * d] = dv[d][r];
-      }
-    return;
-  }
-  // each wave turns its two blocks of 32 keys in its own piece of LDS, one after the other, and writes whole pieces of rows
-  unsigned char *stage = lds + kg * 32 * K::ST;
+      for (int r = 0; r < 16; ++r) sums[(d * 16 + r) * 64] = qg ? dk[d][r] : dv[d][r];
+    __syncthreads();
 #pragma unroll
-  for (int which = 0; which < 2; ++which) {
+    for (int d = 0; d < C::DB; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) dk[d][r] = (qg ? dv[d][r] : dk[d][r]) + theirs[(d * 16 + r) * 64];
+    __syncthreads();
+  }
+  const float mk = all_single ? 0.0f : p.scale;
+  unsigned char *stage = lds + wave * 32 * K::ST;
+#pragma unroll
+  for (int k = 0; k < 2 / K::QG; ++k) {
+    const int which = K::QG > 1 ? qg : k;         // dK or dV
+    f32x16(&acc)[C::DB] = K::QG > 1 || k == 0 ? dk : dv;
+    const float mul = which ? 1.0f : mk;
+    if (split) {     // [part of the launch][dK, dV][key][column] in fp32
+      GPP_G float *part = p.partial + ((int64_t)w.slot * 2 + which) * WIN_ROWS * DH + (int64_t)(32 * kg) * DH + (lane & 31);
+#pragma unroll
+      for (int d = 0; d < C::DB; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) part[win_acc_row(r) * DH + 32 * d] = acc[d][r] * mul;
+      continue;
+    }
+    // a wave turns its block of 32 keys in its own piece of LDS and writes whole pieces of rows
 #pragma unroll
     for (int d = 0; d < C::DB; ++d)
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         T *to = (T *)(stage + win_acc_row(r) * K::ST) + 32 * d + (lane & 31);
-        const float v = which ? dv[d][r] : dk[d][r] * mk;
-        if constexpr (sizeof(T) == 2) *to = f32_to_bf16_bits(v);
-        else *to = v;
+        if constexpr (sizeof(T) == 2) *to = f32_to_bf16_bits(acc[d][r] * mul);
+        else *to = acc[d][r] * mul;
       }
     __builtin_amdgcn_wave_barrier();
     for (int c = lane; c < 32 * (DH / C::EPC); c += 64) {
-      const int row = c / (DH / C::EPC), k = c % (DH / C::EPC);
-      if (k * C::EPC >= p.dh || k0 + row >= p.seq) continue;
-      u32x4 v = *(const u32x4 *)(stage + row * K::ST + k * 16);
+      const int row = c / (DH / C::EPC), x = c % (DH / C::EPC);
+      if (x * C::EPC >= p.dh || k0 + row >= p.seq) continue;
+      u32x4 v = *(const u32x4 *)(stage + row * K::ST + x * 16);
       if (k0 + row >= len) v = (u32x4){0u, 0u, 0u, 0u};
-      *(GPP_G u32x4 *)((GPP_G T *)dqkv + (row0 + k0 + row) * p.ld_out + (which ? vcol : kcol) + k * C::EPC) = v;
+      *(GPP_G u32x4 *)((GPP_G T *)dqkv + (row0 + k0 + row) * p.ld_out + (which ? vcol : kcol) + x * C::EPC) = v;
     }
     __builtin_amdgcn_wave_barrier();
   }
