@@ -63,7 +63,12 @@ struct WinFrag<uint16_t> {
     for (int e = 0; e < 8; ++e) r[e] = (bf16_t)v[8 * c + e];
     return r;
   }
-  static __device__ __forceinline__ float get(const bf16x8 &a, int e) { return (float)a[e]; }
+  static __device__ __forceinline__ float dot(const bf16x8 &a, const bf16x8 &b, float c) {
+    typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) c = __builtin_amdgcn_fdot2_f32_bf16((bf16x2){a[e], a[e + 1]}, (bf16x2){b[e], b[e + 1]}, c, false);
+    return c;
+  }
 };
 template <>
 struct WinFrag<float> {
@@ -80,7 +85,11 @@ struct WinFrag<float> {
     for (int e = 0; e < 8; ++e) r[e] = v[8 * c + e];
     return r;
   }
-  static __device__ __forceinline__ float get(const f32x8 &a, int e) { return a[e]; }
+  static __device__ __forceinline__ float dot(const f32x8 &a, const f32x8 &b, float c) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) c = fmaf(a[e], b[e], c);
+    return c;
+  }
 };
 
 // operand rows that a wave keeps: lane's row, columns 16 s + 8 (l / 32) .. of step s; columns beyond the head are zero
@@ -308,7 +317,8 @@ struct WinKeyStream {
     whole = win_tile_bytes(C::KT, ld, dh, C::ES);
     tail = win_tile_bytes((len - 1) % C::KT + 1, ld, dh, C::ES);
   }
-  __device__ __forceinline__ void copy(const WinCopy<T, DH, 4> &co, uint32_t dst, int wave) {
+  template <int NW>
+  __device__ __forceinline__ void copy(const WinCopy<T, DH, NW> &co, uint32_t dst, int wave) {
     const uint32_t bytes = rows >= C::KT ? whole : tail;
     rsrc4 rk = win_rsrc(k, bytes), rv = win_rsrc(k + v, bytes);
     settle(rk, rv);
@@ -420,23 +430,23 @@ struct WinKeep {
   }
 };
 
-// A wave owns 32 queries.  KG = 1: four waves, 128 queries.  KG = 2: two waves share their queries and take one half of every tile of
-// keys each, 64 queries per workgroup; for launches of so few blocks that they would leave compute units idle.
-template <typename T, int DH>
+// A wave owns 32 queries.  KG = 1: a wave for every 32.  KG = 2: two waves share their queries and take one half of every tile of keys
+// each; for launches of so few blocks that they would leave compute units idle.
+template <typename T, int DH, int NW, int KG>
 struct WinQueryCfg {
   typedef WinTile<T, DH> C;
+  static constexpr int QG = NW / KG, ROWS = 32 * QG;
   static constexpr int NB = C::RB == 128 ? 3 : 2;                                  // buffers: as many as leave room for two workgroups' waves
-  static constexpr int CP = 2 * C::KT / C::RPG / 4;                                // copies of a wave per step
-  static constexpr int OUT = 128 * (DH * C::ES + 16), JOIN = 2 * 32 * (DH + 2) * 4;
+  static constexpr int CP = 2 * C::KT / C::RPG / NW;                               // copies of a wave per step
+  static constexpr int OUT = ROWS * (DH * C::ES + 16), JOIN = KG == 2 ? QG * 32 * (DH + 2) * 4 : 0;
   static constexpr int TILES = 2 * NB * C::BYTES, LDS = TILES > OUT ? (TILES > JOIN ? TILES : JOIN) : (OUT > JOIN ? OUT : JOIN);
 };
 
 // What forward and dQ do with their tiles of K and V: a ring of NB buffers; step(K tile, V tile, first key)
-template <typename T, int DH, typename Step>
+template <typename Q, typename T, int DH, int NW, typename Step>
 __device__ __forceinline__ void win_stream_keys(const WinRange &tiles, int nt, WinKeyStream<T, DH> &stream, const unsigned char *lds, int wave,
-                                                const WinCopy<T, DH, 4> &co, uint32_t lds0, const Step &step) {
+                                                const WinCopy<T, DH, NW> &co, uint32_t lds0, const Step &step) {
   typedef WinTile<T, DH> C;
-  typedef WinQueryCfg<T, DH> Q;
   uint32_t in = 2 * (Q::NB - 1) * C::BYTES, out = 0;       // buffers of the next copy and of this step
   for (int t = 0; t < nt; ++t) {
     if (Q::NB > 2 && t + Q::NB - 1 <= nt) copies_landed_barrier<(Q::NB - 2) * Q::CP>();
@@ -455,14 +465,14 @@ template <typename T, int DH, int KG>
 __global__ __launch_bounds__(256, 2) void k_window_fwd_mfma(const WindowProb *__restrict__ probs, int n, ExtPtrs ext, StageFlags *flags) {
   typedef WinTile<T, DH> C;
   typedef WinFrag<T> F;
-  typedef WinQueryCfg<T, DH> Q;
-  constexpr int ROWS = 128 / KG;
+  typedef WinQueryCfg<T, DH, 4, KG> Q;
+  constexpr int ROWS = Q::ROWS;
   __shared__ __attribute__((aligned(16))) unsigned char lds[Q::LDS];
   const int pi = find_prob(probs, n, blockIdx.x);
   const WindowProb p = probs[pi];
   win_fetch(p);
   const WinBlock w = win_query_block(p, win_spread(blockIdx.x - p.blk_begin, p.query_units, p.by_run), ROWS);
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), qg = wave & (4 / KG - 1), kg = wave / (4 / KG);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), qg = wave % Q::QG, kg = wave / Q::QG;
   const int len = __builtin_amdgcn_readfirstlane(window_length_checked(p, ext, w.b, w.h == 0 && w.r0 == 0 && threadIdx.x == 0, flags));
   const GPP_G T *qkv = (const GPP_G T *)(p.ext_qkv >= 0 ? ext.p[p.ext_qkv] : p.qkv);
   const int64_t row0 = (int64_t)w.b * p.seq;
@@ -545,7 +555,7 @@ __global__ __launch_bounds__(256, 2) void k_window_fwd_mfma(const WindowProb *__
       for (int d = 0; d < C::DB; ++d) o[d] = F::mma(win_col_frag<T, DH>(at, tv, 16 * c, d), pf, o[d]);
     }
   };
-  win_stream_keys<T, DH>(tiles, tiles.n, stream, lds, wave, co, lds0,
+  win_stream_keys<Q>(tiles, tiles.n, stream, lds, wave, co, lds0,
                          [&](const unsigned char *tk, const unsigned char *tv, int k0) {
     constexpr int N = C::SUB / KG;
     const int u = KG == 1 ? 0 : kg, sees = mine.sees(k0 + 32 * u, 32 * N);
@@ -589,18 +599,15 @@ __global__ __launch_bounds__(256, 2) void k_window_fwd_mfma(const WindowProb *__
 }
 
 // ======================================================================= backward: dQ, and delta = rowsum(dO * O)
-template <typename T, int DH, int KG>
-__global__ __launch_bounds__(256, 2) void k_window_dq_mfma(const WindowProb *__restrict__ probs, int n, ExtPtrs ext) {
+// (`local`: block of queries of the record; `lds`: Q::LDS bytes.  DELTA: the deltas are written for the dK / dV kernel behind this one)
+template <typename T, int DH, int NW, int KG, bool DELTA>
+__device__ __forceinline__ void win_dq_body(const WindowProb &p, const ExtPtrs &ext, int local, unsigned char *lds) {
   typedef WinTile<T, DH> C;
   typedef WinFrag<T> F;
-  typedef WinQueryCfg<T, DH> Q;
-  constexpr int ROWS = 128 / KG;
-  __shared__ __attribute__((aligned(16))) unsigned char lds[Q::LDS];
-  const int pi = find_prob(probs, n, blockIdx.x);
-  const WindowProb p = probs[pi];
-  win_fetch(p);
-  const WinBlock w = win_query_block(p, win_spread(blockIdx.x - p.blk_begin, p.query_units, p.by_run), ROWS);
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), qg = wave & (4 / KG - 1), kg = wave / (4 / KG);
+  typedef WinQueryCfg<T, DH, NW, KG> Q;
+  constexpr int ROWS = Q::ROWS;
+  const WinBlock w = win_query_block(p, win_spread(local, p.query_units, p.by_run), ROWS);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), qg = wave % Q::QG, kg = wave / Q::QG;
   const int len = __builtin_amdgcn_readfirstlane(window_length(p, w.b));
   const GPP_G T *qkv = (const GPP_G T *)p.qkv;
   const int64_t row0 = (int64_t)w.b * p.seq;
@@ -609,7 +616,7 @@ __global__ __launch_bounds__(256, 2) void k_window_dq_mfma(const WindowProb *__r
   const WinRange tiles = win_range<C::KT>(p, w.r0, min(w.r0 + ROWS, len) - 1, len);
   GPP_G void *dqkv = p.ext_out >= 0 ? (GPP_G void *)ext.p[p.ext_out] : p.out;
   const int nt = dqkv ? tiles.n : 0;
-  const WinCopy<T, DH, 4> co = win_copy_offsets<T, DH, 4>(wave, p.ld_qkv, p.dh);
+  const WinCopy<T, DH, NW> co = win_copy_offsets<T, DH, NW>(wave, p.ld_qkv, p.dh);
   const uint32_t lds0 = lds_address((const uint16_t *)lds);
   WinKeyStream<T, DH> stream(kbase, (int64_t)p.kv_heads * p.dh, p.ld_qkv, p.dh, tiles, len);
 #pragma unroll
@@ -622,11 +629,9 @@ __global__ __launch_bounds__(256, 2) void k_window_dq_mfma(const WindowProb *__r
   {
     const WinRows<T, DH> of = win_rows<T, DH>(p.o, row0 + qc, p.ld_o, (int64_t)w.h * p.dh, p.dh);
 #pragma unroll
-    for (int s = 0; s < C::KS; ++s)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) delta = fmaf(F::get(gf.f[s], e), F::get(of.f[s], e), delta);
+    for (int s = 0; s < C::KS; ++s) delta = F::dot(gf.f[s], of.f[s], delta);
     delta = win_half_sum(delta);
-    if (kg == 0 && lane < 32 && q < len) p.delta[stat] = -delta;      // (as the dK / dV kernel takes it)
+    if (DELTA && kg == 0 && lane < 32 && q < len) p.delta[stat] = -delta;      // (as the dK / dV kernel takes it)
   }
   const WinLane<T, DH> at = win_lane<T, DH>();
   const WinWave mine = win_wave(p, q0, len);
@@ -638,7 +643,7 @@ __global__ __launch_bounds__(256, 2) void k_window_dq_mfma(const WindowProb *__r
 #pragma unroll
   for (int d = 0; d < C::DB; ++d) dq[d] = win_zero();
 
-  win_stream_keys<T, DH>(tiles, nt, stream, lds, wave, co, lds0,
+  win_stream_keys<Q>(tiles, nt, stream, lds, wave, co, lds0,
                          [&](const unsigned char *tk, const unsigned char *tv, int k0) {
 #pragma unroll
     for (int u = 0; u < C::SUB; ++u) {
@@ -689,6 +694,15 @@ __global__ __launch_bounds__(256, 2) void k_window_dq_mfma(const WindowProb *__r
   }
   if (kg == 0)
     win_store_rows<T, DH>(lds, qg, dq, p.scale, q0, len, p.seq, p.dh, dqkv, row0, p.ld_out, nullptr, 0, (int64_t)w.h * p.dh);
+}
+
+template <typename T, int DH, int KG>
+__global__ __launch_bounds__(256, 2) void k_window_dq_mfma(const WindowProb *__restrict__ probs, int n, ExtPtrs ext) {
+  __shared__ __attribute__((aligned(16))) unsigned char lds[WinQueryCfg<T, DH, 4, KG>::LDS];
+  const int pi = find_prob(probs, n, blockIdx.x);
+  const WindowProb p = probs[pi];
+  win_fetch(p);
+  win_dq_body<T, DH, 4, KG, true>(p, ext, blockIdx.x - p.blk_begin, lds);
 }
 
 // ======================================================================= backward: dK, dV
@@ -746,32 +760,28 @@ __device__ __forceinline__ WinSteps win_steps(const WindowProb &p, int c0, int l
 // other's chains (LDS reads -> score products -> exponentials -> gradient products), and add their sums at the end.  Two waves have 256
 // registers each; with heads of more than 64 columns the sums take 128 of them, so V is then read from LDS like the tiles, K stays
 // in registers.
-template <typename T, int DH>
+// OWN: the deltas are formed here, from a tile of O beside the one of dO, instead of read from the dQ kernel in front of this one.
+template <typename T, int DH, bool OWN>
 struct WinKeyCfg {
   typedef WinTile<T, DH> C;
-  static constexpr int QG = C::SUB, NW = 4 * QG, BUF = 2 * C::BYTES + 1024;      // Q, dO, and the log-sum-exps and deltas of the tile's queries
+  static constexpr int QG = C::SUB, NW = 4 * QG;
+  static constexpr int STAT = (OWN ? 3 : 2) * C::BYTES, BUF = STAT + 1024;       // Q, dO (and O), the log-sum-exps and deltas of the tile's queries
   static constexpr bool V_LDS = sizeof(T) == 2 && DH > 64;
   static constexpr int V_BYTES = V_LDS ? WIN_ROWS / C::RPG * C::GROUP : 0, ST = DH * C::ES + 16;
   static constexpr int JOIN = QG > 1 ? NW * 32 * DH * 4 : 0, OUT = NW * 32 * ST;    // over the tiles: a half of every wave's sums, rows of the result
-  static constexpr int NB = C::RB == 128 ? 4 : (DH * C::ES > 256 ? 2 : 3);         // buffers, as many as the LDS of a compute unit's workgroups holds
-  static constexpr int CP = 2 * C::KT / C::RPG / NW;                               // copies of a wave per step, at least
-  static constexpr int TILES = NB * BUF + V_BYTES, LDS = TILES > JOIN ? (TILES > OUT ? TILES : OUT) : (JOIN > OUT ? JOIN : OUT);
+  static constexpr int NB = C::RB == 128 ? 4 : (DH * C::ES > 256 || OWN ? 2 : 3);  // buffers, as many as the LDS of a compute unit's workgroups holds
+  static constexpr int CP = (OWN ? 3 : 2) * C::KT / C::RPG / NW;                               // copies of a wave per step, at least
+  static constexpr int TILES = NB * BUF + V_BYTES + (OWN ? NW * 128 : 0), LDS = TILES > JOIN ? (TILES > OUT ? TILES : OUT) : (JOIN > OUT ? JOIN : OUT);
 };
 
-template <typename T, int DH>
-__global__ __launch_bounds__((WinKeyCfg<T, DH>::NW * 64), (DH * sizeof(T) <= 256 ? 2 : 1)) void k_window_dkv_mfma(const WindowProb *__restrict__ probs, int n,
-                                                                                                       ExtPtrs ext) {
+template <typename T, int DH, bool OWN>
+__device__ __forceinline__ void win_dkv_body(const WindowProb &p, const ExtPtrs &ext, int local, unsigned char *lds) {
   typedef WinTile<T, DH> C;
   typedef WinFrag<T> F;
-  typedef WinKeyCfg<T, DH> K;
-  __shared__ __attribute__((aligned(16))) unsigned char lds[K::LDS];
-  const int pi = find_prob(probs, n, blockIdx.x);
-  const WindowProb p = probs[pi];
-  win_fetch(p);
+  typedef WinKeyCfg<T, DH, OWN> K;
   GPP_G void *dqkv = p.ext_out >= 0 ? (GPP_G void *)ext.p[p.ext_out] : p.out;
   if (!dqkv) return;
   // (the unsplit units first, then the others)
-  const int local = blockIdx.x - p.blk_begin;
   const WinUnit w = win_unit(p, local < p.whole ? win_spread(local, p.whole, p.by_key_blocks) : p.whole + win_spread(local - p.whole, p.units - p.whole, p.by_key_blocks));
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), kg = wave & 3, qg = wave >> 2;
   const int len = __builtin_amdgcn_readfirstlane(window_length(p, w.b));
@@ -787,14 +797,18 @@ __global__ __launch_bounds__((WinKeyCfg<T, DH>::NW * 64), (DH * sizeof(T) <= 256
   const int k0 = w.c0 + 32 * kg, k1 = min(k0 + 31, len - 1), kc = max(0, min(k0 + (lane & 31), len - 1));
   const int64_t kcol = (int64_t)(p.heads + w.g) * p.dh, vcol = kcol + (int64_t)p.kv_heads * p.dh;
   const WinCopy<T, DH, K::NW> cq = win_copy_offsets<T, DH, K::NW>(wave, p.ld_qkv, p.dh), cg = win_copy_offsets<T, DH, K::NW>(wave, p.ld_dout, p.dh);
+  const WinCopy<T, DH, K::NW> cw = win_copy_offsets<T, DH, K::NW>(wave, OWN ? p.ld_o : 0, p.dh);      // (O's)
   const uint32_t lds0 = lds_address((const uint16_t *)lds);
   // of the next step to be copied: tile of its head, rows of the sample from there on, Q, dO, and (wave 0, 1) log-sum-exps or deltas
   int head = s0 < s1 ? s0 / nt : 0, tile = s0 - head * nt, rows = len - (t0 + tile) * C::KT;
   const GPP_G T *qn = qkv + (row0 + (t0 + tile) * C::KT) * p.ld_qkv + (int64_t)(h0 + head) * p.dh;
   const GPP_G T *gn = dout + (row0 + (t0 + tile) * C::KT) * p.ld_dout + (int64_t)(h0 + head) * p.dh;
+  const GPP_G T *on = OWN ? (const GPP_G T *)p.o + (row0 + (t0 + tile) * C::KT) * p.ld_o + (int64_t)(h0 + head) * p.dh : nullptr;
   const GPP_G float *sn = (wave == 0 ? p.lse : p.delta) + ((int64_t)w.b * p.heads + h0 + head) * p.seq + (t0 + tile) * C::KT;
   const int64_t q_step = C::KT * p.ld_qkv, g_step = C::KT * p.ld_dout;
   const uint32_t q_whole = win_tile_bytes(C::KT, p.ld_qkv, p.dh, C::ES), q_tail = win_tile_bytes((len - 1) % C::KT + 1, p.ld_qkv, p.dh, C::ES);
+  const int64_t o_step = C::KT * p.ld_o;
+  const uint32_t o_whole = win_tile_bytes(C::KT, p.ld_o, p.dh, C::ES), o_tail = win_tile_bytes((len - 1) % C::KT + 1, p.ld_o, p.dh, C::ES);
   const uint32_t g_whole = win_tile_bytes(C::KT, p.ld_dout, p.dh, C::ES), g_tail = win_tile_bytes((len - 1) % C::KT + 1, p.ld_dout, p.dh, C::ES);
   auto copy_next = [&](int buf) {
     const bool full = rows >= C::KT;
@@ -802,10 +816,16 @@ __global__ __launch_bounds__((WinKeyCfg<T, DH>::NW * 64), (DH * sizeof(T) <= 256
     settle(rq, rg);
     win_copy(rq, cq, lds0 + buf * K::BUF, wave);
     win_copy(rg, cg, lds0 + buf * K::BUF + C::BYTES, wave);
-    if (wave < 2) {      // (queries behind the end: zero, as their rows)
+    if constexpr (OWN) {
+      rsrc4 ro = win_rsrc(on, full ? o_whole : o_tail), same = ro;
+      settle(ro, same);
+      win_copy(ro, cw, lds0 + buf * K::BUF + 2 * C::BYTES, wave);
+      on += o_step;
+    }
+    if (wave < (OWN ? 1 : 2)) {      // (queries behind the end: zero, as their rows)
       rsrc4 rs = win_rsrc(sn, (uint32_t)min(rows, C::KT) * 4), same = rs;
       settle(rs, same);
-      lds_copy4(rs, lds0 + buf * K::BUF + 2 * C::BYTES + wave * 512, lane * 4);
+      lds_copy4(rs, lds0 + buf * K::BUF + K::STAT + wave * 512, lane * 4);
     }
     qn += q_step;
     gn += g_step;
@@ -815,6 +835,7 @@ __global__ __launch_bounds__((WinKeyCfg<T, DH>::NW * 64), (DH * sizeof(T) <= 256
       tile = 0;
       qn += p.dh - nt * q_step;
       gn += p.dh - nt * g_step;
+      if (OWN) on += p.dh - nt * o_step;
       sn += p.seq - nt * C::KT;
       rows += nt * C::KT;
     }
@@ -866,19 +887,37 @@ __global__ __launch_bounds__((WinKeyCfg<T, DH>::NW * 64), (DH * sizeof(T) <= 256
     now = now + 1 == nt ? 0 : now + 1;
     if (i0 >= any_end || i0 + 32 <= any_first) continue;
     const bool all = i0 >= all_first && min(i0 + 32, len) <= all_end;
-    const float *tl = (const float *)(tq + 2 * C::BYTES) + 32 * qg + 4 * (lane >> 5), *td = tl + 128;
-    f32x16 st = win_zero(), dp;      // (dP - delta: the products are added to -delta)
+    const float *tl = (const float *)(tq + K::STAT) + 32 * qg + 4 * (lane >> 5), *td = tl + 128;
+    f32x16 st = win_zero(), dp = win_zero();
+    if constexpr (!OWN) {      // dP - delta: the products are added to -delta
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const f32x4 minus = *(const f32x4 *)(td + 8 * k);
+      for (int k = 0; k < 4; ++k) {
+        const f32x4 minus = *(const f32x4 *)(td + 8 * k);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) dp[4 * k + e] = minus[e];
+        for (int e = 0; e < 4; ++e) dp[4 * k + e] = minus[e];
+      }
     }
+    float own = 0.0f;
 #pragma unroll
     for (int x = 0; x < C::KS; ++x) {
       st = F::mma(win_row_frag<T, DH>(at, tq + C::at(32) * qg, 0, x), kf.f[x], st);
-      if constexpr (K::V_LDS) dp = F::mma(win_row_frag<T, DH>(at, tg + C::at(32) * qg, 0, x), win_row_frag<T, DH>(at, lds + K::NB * K::BUF + C::at(32) * kg, 0, x), dp);
-      else dp = F::mma(win_row_frag<T, DH>(at, tg + C::at(32) * qg, 0, x), vf.f[x], dp);
+      const typename F::type g = win_row_frag<T, DH>(at, tg + C::at(32) * qg, 0, x);
+      if constexpr (K::V_LDS) dp = F::mma(g, win_row_frag<T, DH>(at, lds + K::NB * K::BUF + C::at(32) * kg, 0, x), dp);
+      else dp = F::mma(g, vf.f[x], dp);
+      if constexpr (OWN) own = F::dot(g, win_row_frag<T, DH>(at, tg + C::BYTES + C::at(32) * qg, 0, x), own);
+    }
+    if constexpr (OWN) {       // of the lane's row; through a piece of LDS of the wave's own to the rows that the lane holds of the product
+      float *mine = (float *)(lds + K::NB * K::BUF + K::V_BYTES) + 32 * wave;
+      own = win_half_sum(own);
+      if (lane < 32) mine[lane] = own;
+      __builtin_amdgcn_wave_barrier();
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const f32x4 delta = *(const f32x4 *)(mine + 4 * (lane >> 5) + 8 * k);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) dp[4 * k + e] -= delta[e];
+      }
+      __builtin_amdgcn_wave_barrier();
     }
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
@@ -962,6 +1001,32 @@ __global__ __launch_bounds__((WinKeyCfg<T, DH>::NW * 64), (DH * sizeof(T) <= 256
   }
 }
 
+template <typename T, int DH>
+__global__ __launch_bounds__((WinKeyCfg<T, DH, false>::NW * 64), (DH * sizeof(T) <= 256 ? 2 : 1)) void k_window_dkv_mfma(const WindowProb *__restrict__ probs,
+                                                                                                              int n, ExtPtrs ext) {
+  __shared__ __attribute__((aligned(16))) unsigned char lds[WinKeyCfg<T, DH, false>::LDS];
+  const int pi = find_prob(probs, n, blockIdx.x);
+  const WindowProb p = probs[pi];
+  win_fetch(p);
+  win_dkv_body<T, DH, false>(p, ext, blockIdx.x - p.blk_begin, lds);
+}
+
+// Small problems: dK / dV and dQ side by side in one launch, first the blocks of keys, then those of queries.  A launch of few
+// workgroups is as long as the chain of one of them, and together they still find a compute unit each.
+template <typename T, int DH>
+__global__ __launch_bounds__((WinKeyCfg<T, DH, true>::NW * 64), (DH * sizeof(T) <= 256 ? 2 : 1)) void k_window_bwd_mfma(const WindowProb *__restrict__ probs,
+                                                                                                             int n, ExtPtrs ext) {
+  typedef WinKeyCfg<T, DH, true> K;
+  typedef WinQueryCfg<T, DH, K::NW, WinTile<T, DH>::SUB> Q;
+  __shared__ __attribute__((aligned(16))) unsigned char lds[K::LDS > Q::LDS ? K::LDS : Q::LDS];
+  const int pi = find_prob(probs, n, blockIdx.x);
+  const WindowProb p = probs[pi];
+  win_fetch(p);
+  const int local = blockIdx.x - p.blk_begin;
+  if (local < p.units) win_dkv_body<T, DH, true>(p, ext, local, lds);
+  else win_dq_body<T, DH, K::NW, WinTile<T, DH>::SUB, false>(p, ext, local - p.units, lds);
+}
+
 // The sums of a split block's parts, in order: four columns of a key per thread, DH / 4 workgroups per block
 template <typename T, int DH>
 __global__ __launch_bounds__(256) void k_window_join(const WindowProb *__restrict__ probs, int n, ExtPtrs ext) {
@@ -1017,17 +1082,14 @@ int window_mfma_dh(const WindowProb &p) {
 static int window_tile_rows(const WindowProb &p, int dh) { return dh * (p.dtype == DT_BF16 ? 2 : 4) > 256 ? 32 : 64; }
 // Two waves per 32 queries where the blocks of 128 are at most two per compute unit
 int window_key_groups(const WindowProb &p, int dh, int64_t blocks) { return window_tile_rows(p, dh) == 64 && blocks <= 512 ? 2 : 1; }
-int window_mfma_query_blocks(const WindowProb &p, int key_groups) {
-  const int rows = WIN_ROWS / key_groups;
-  return p.batch * p.heads * ((p.seq + rows - 1) / rows);
-}
-void window_plan_queries(WindowProb &p, int key_groups) {
-  const int rows = WIN_ROWS / key_groups;
+// whether the backward pass is one launch: its workgroups, one per compute unit, all run at once
+bool window_one_backward(int64_t workgroups) { return workgroups <= 256; }
+void window_plan_queries(WindowProb &p, int rows) {
   p.by_group = fast_div(p.heads / p.kv_heads);
   p.by_kv_heads = fast_div(p.kv_heads);
   p.by_query_blocks = fast_div((p.seq + rows - 1) / rows);
   p.by_run = fast_div((int64_t)p.by_group.d * p.by_query_blocks.d);
-  p.query_units = window_mfma_query_blocks(p, key_groups);
+  p.query_units = (int32_t)((int64_t)p.batch * p.heads * ((p.seq + rows - 1) / rows));
 }
 
 // Cuts the key blocks of a launch (see WinUnit) into units, of which `slots` run at once: the first `whole` blocks stay in one piece,
@@ -1035,8 +1097,8 @@ void window_plan_queries(WindowProb &p, int key_groups) {
 // gaps that whole blocks leave.  Of the pairs (whole, part_steps) the one with the least estimate, in steps: what a slot has to do, but
 // no less than the rounds of whole blocks, plus half a part of unevenness; a unit costs the time of some steps for its operands
 // and its result (4 us: about four steps of 64 x 128 pairs in bf16, half a one in fp32), a part its sums' way through memory, the
-// joining launch (5 us) the same for all.
-void window_plan_parts(WindowProb &p, int dh, int slots) {
+// joining launch (5 us) the same for all.  one_round: no more units than slots, if there is such a pair (units = 0: there is none).
+void window_plan_parts(WindowProb &p, int dh, int slots, bool one_round) {
   const int64_t kt = window_tile_rows(p, dh), group = p.heads / p.kv_heads, seq = p.seq, nb = (seq + WIN_ROWS - 1) / WIN_ROWS;
   const int64_t win = p.window ? std::min<int64_t>(p.window, seq) : seq, bg = (int64_t)p.batch * p.kv_heads;
   const int64_t sb = p.window ? (std::min<int64_t>(p.sinks, seq) + WIN_ROWS - 1) / WIN_ROWS : 0;
@@ -1046,6 +1108,7 @@ void window_plan_parts(WindowProb &p, int dh, int slots) {
   auto up = [](int64_t v, int64_t by) { return (v + by - 1) / by; };
   const double start = p.dtype == DT_BF16 ? 4.0 : 0.5, join = p.dtype == DT_BF16 ? 6.0 : 0.75, sums = p.dtype == DT_BF16 ? 0.00035 * dh : 0.00005 * dh;
   double best = 1e300;
+  p.units = 0;
   for (int64_t whole = blocks;; whole = std::max<int64_t>(0, std::min(whole - 1, whole - slots / 8) / 8 * 8)) {
     for (int64_t part = p.dtype == DT_BF16 ? 8 : 1; part < 2 * every + 8; part += part < 8 ? 1 : (part < 32 ? 4 : part / 8)) {
       const int64_t rest = blocks - whole, parts = up(regular, part), sink_parts = sb ? up(every, part) : 1;
@@ -1056,7 +1119,7 @@ void window_plan_parts(WindowProb &p, int dh, int slots) {
       const double longest = std::max((double)(whole ? regular : 0), (double)std::min(part, std::max(rest ? regular : 0, sb ? every : 0))) + start;
       const double rounds = triangle ? longest : (double)up(whole, slots) * (regular + start);
       const double t = std::max(std::max(slot, longest), rounds) + 0.5 * (split ? (double)part : 0.0) + (split ? join + sums * (double)split : 0.0);
-      if (t >= best) continue;
+      if (t >= best || (one_round && units > slots)) continue;
       best = t;
       p.whole = (int32_t)whole;
       p.part_steps = (int32_t)part;
@@ -1117,7 +1180,13 @@ void launch_window_dq_mfma(const WindowProb *probs, int n, int total_blocks, int
 }
 void launch_window_dkv_mfma(const WindowProb *probs, int n, int total_blocks, int dtype, int dh, const ExtPtrs &ext, hipStream_t s) {
   if (total_blocks <= 0) return;
-#define GO(T, DH) hipLaunchKernelGGL((k_window_dkv_mfma<T, DH>), dim3(total_blocks), dim3((WinKeyCfg<T, DH>::NW * 64)), 0, s, probs, n, ext)
+#define GO(T, DH) hipLaunchKernelGGL((k_window_dkv_mfma<T, DH>), dim3(total_blocks), dim3((WinKeyCfg<T, DH, false>::NW * 64)), 0, s, probs, n, ext)
+  WIN_INSTANCE(GO);
+#undef GO
+}
+void launch_window_bwd_mfma(const WindowProb *probs, int n, int total_blocks, int dtype, int dh, const ExtPtrs &ext, hipStream_t s) {
+  if (total_blocks <= 0) return;
+#define GO(T, DH) hipLaunchKernelGGL((k_window_bwd_mfma<T, DH>), dim3(total_blocks), dim3((WinKeyCfg<T, DH, true>::NW * 64)), 0, s, probs, n, ext)
   WIN_INSTANCE(GO);
 #undef GO
 }

@@ -378,9 +378,9 @@ int window_max_head_dim();
 int window_mfma_dh(const WindowProb &p);
 // key groups of a launch of `blocks` blocks of 128 queries: how many waves share 32 queries
 int window_key_groups(const WindowProb &p, int dh, int64_t blocks);
-void window_plan_queries(WindowProb &p, int key_groups);
-int window_mfma_query_blocks(const WindowProb &p, int key_groups);
-void window_plan_parts(WindowProb &p, int dh, int slots);
+bool window_one_backward(int64_t workgroups);
+void window_plan_queries(WindowProb &p, int rows);      // blocks of `rows` queries
+void window_plan_parts(WindowProb &p, int dh, int slots, bool one_round);
 int window_key_slots(int dtype, int dh);
 int window_mfma_key_blocks(const WindowProb &p);
 int window_join_blocks(const WindowProb &p, int dh);
@@ -388,6 +388,7 @@ int64_t window_partial_bytes(const WindowProb &p, int dh);
 void launch_window_fwd_mfma(const WindowProb *probs, int n, int total_blocks, int dtype, int dh, int key_groups, const ExtPtrs &ext, StageFlags *flags, hipStream_t s);
 void launch_window_dq_mfma(const WindowProb *probs, int n, int total_blocks, int dtype, int dh, int key_groups, const ExtPtrs &ext, hipStream_t s);
 void launch_window_dkv_mfma(const WindowProb *probs, int n, int total_blocks, int dtype, int dh, const ExtPtrs &ext, hipStream_t s);
+void launch_window_bwd_mfma(const WindowProb *probs, int n, int total_blocks, int dtype, int dh, const ExtPtrs &ext, hipStream_t s);
 void launch_window_join(const WindowProb *probs, int n, int total_blocks, int dtype, int dh, const ExtPtrs &ext, hipStream_t s);
 int window_blocks(int64_t batch, int heads, int seq);
 

@@ -790,17 +790,32 @@ struct Emitter {
           if (a.dtype == dt && mfma_dh(a) == dh) now.push_back(a);
         if (now.empty()) continue;
         int64_t blocks128 = 0;
-        for (auto &a : now) blocks128 += window_mfma_query_blocks(a, 1);
+        for (auto &a : now) blocks128 += (int64_t)a.batch * a.heads * ((a.seq + 127) / 128);
         const int groups = dh ? window_key_groups(now[0], dh, blocks128) : 1;
-        for (auto &a : now) window_plan_queries(a, groups);
-        auto queries = [&](const WindowProb &a) { return dh ? window_mfma_query_blocks(a, groups) : window_blocks(a.batch, a.heads, a.seq); };
+        // (the branches of a level share the GPU; in one launch the blocks of keys take what the blocks of 128 queries leave)
+        bool one = dh && backward && window_one_backward(2 * blocks128);
+        auto plan_keys = [&] {
+          const int slots = std::max(1, (int)((one ? 256 - blocks128 : window_key_slots(dt, dh)) / (int64_t)now.size()));
+          bool fits = true;
+          for (auto &a : now) {
+            window_plan_queries(a, 128);
+            window_plan_parts(a, dh, one ? slots : std::max(8, slots / 8 * 8), one);
+            fits = fits && a.units > 0;
+          }
+          return fits;
+        };
+        if (dh && backward && !plan_keys()) {
+          one = false;
+          plan_keys();
+        }
+        for (auto &a : now) window_plan_queries(a, one ? 128 : 128 / groups);
+        auto queries = [&](const WindowProb &a) { return dh ? a.query_units : window_blocks(a.batch, a.heads, a.seq); };
         if (!backward) {
           step(K_WINDOW_FWD, now, dt, dh, groups, queries);
           continue;
         }
         if (dh)
-          for (auto &a : now) {      // (the branches of a level share the GPU)
-            window_plan_parts(a, dh, std::max(8, window_key_slots(dt, dh) / (int)now.size() / 8 * 8));
+          for (auto &a : now) {
             const int64_t bytes = window_partial_bytes(a, dh);
             if (bytes == 0) continue;
             Buf b;
@@ -809,6 +824,11 @@ struct Emitter {
             shared_tmp_top = align_up(shared_tmp_top + bytes, 256);
             a.partial = (float *)ptr(b);
           }
+        if (one) {
+          step(K_WINDOW_BWD, now, dt, dh, 1, [&](const WindowProb &a) { return a.units + a.query_units; });
+          step(K_WINDOW_JOIN, now, dt, dh, 1, [&](const WindowProb &a) { return window_join_blocks(a, dh); });
+          continue;
+        }
         step(K_WINDOW_DQ, now, dt, dh, groups, queries);
         step(K_WINDOW_DKV, now, dt, dh, 1, [&](const WindowProb &a) { return dh ? window_mfma_key_blocks(a) : window_blocks(a.batch, a.kv_heads, a.seq); });
         if (dh) step(K_WINDOW_JOIN, now, dt, dh, 1, [&](const WindowProb &a) { return window_join_blocks(a, dh); });

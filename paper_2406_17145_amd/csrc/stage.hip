@@ -107,7 +107,7 @@ static int step_tag(const Step &sp, bool backward) {
     case K_ROTARY: return backward ? 7 : 6;
     case K_ATTN_FWD: case K_WINDOW_FWD: return 12;
     case K_ATTN_DQ: case K_WINDOW_DQ: return 13;
-    case K_ATTN_DKV: case K_WINDOW_DKV: case K_WINDOW_JOIN: return 14;
+    case K_ATTN_DKV: case K_WINDOW_DKV: case K_WINDOW_BWD: case K_WINDOW_JOIN: return 14;
     case K_POOL: return backward ? 16 : 15;
     case K_EMB_FWD: return 17;
     case K_EMB_BWD: return 18;
@@ -551,6 +551,7 @@ static gpp_status_t run_steps(gpp_stage *st, const std::vector<Step> &steps, int
         if (sp.a1) launch_window_dkv_mfma((const WindowProb *)tab, sp.n, sp.blocks, sp.a0, sp.a1, ext, s);
         else launch_window_dkv((const WindowProb *)tab, sp.n, sp.blocks, ext, s);
         break;
+      case K_WINDOW_BWD: launch_window_bwd_mfma((const WindowProb *)tab, sp.n, sp.blocks, sp.a0, sp.a1, ext, s); break;
       case K_WINDOW_JOIN: launch_window_join((const WindowProb *)tab, sp.n, sp.blocks, sp.a0, sp.a1, ext, s); break;
       case K_POOL: launch_pool((const PoolProb *)tab, sp.n, sp.blocks, s); break;
       case K_EMB_FWD: launch_emb_fwd((const EmbProb *)tab, sp.n, sp.blocks, sp.a0, sp.a1, flags, s); break;

@@ -175,13 +175,16 @@ def _launches(ops, b):
 
 
 def test_a_stage_of_one_operator_works_on_the_callers_tensors(lib):
-    """No copies in or out: two launches for a rotary, forward, delta and dQ, dK and dV for an attention (whose forward launch keeps Q, K and V)."""
+    """No copies in or out: two launches for a rotary, for an attention forward (which keeps Q, K and V)
+    and backward, the gradients in one launch of few workgroups or two."""
     steps, size = _launches(S.rotary_ops(2, 64, 6, 64, (8, 12, 12), rest=128), 2)
     assert steps == [("forward", "elt_fwd"), ("backward", "elt_bwd")]
     assert size < 64 * 1024          # positions (rows padded to 64) and tables: no tensor of [128, 512]
     steps, size = _launches(S.attention_ops(2, 64, 4, 2, 64, window=9, lengths=True, grad=False), 2)
     assert steps == [("forward", "attention_fwd")] and size < 8192
     steps, _ = _launches(S.attention_ops(2, 64, 4, 2, 64, window=9, lengths=True), 2)
+    assert steps == [("forward", "attention_fwd"), ("backward", "attention_bwd_dkv")]
+    steps, _ = _launches(S.attention_ops(16, 1024, 8, 2, 64, window=9), 16)
     assert steps == [("forward", "attention_fwd"), ("backward", "attention_bwd_dq"), ("backward", "attention_bwd_dkv")]
 
 
