@@ -1080,8 +1080,12 @@ int window_mfma_dh(const WindowProb &p) {
   return p.dh <= 32 ? 32 : (p.dh <= 64 ? 64 : (p.dh <= 96 ? 96 : 128));
 }
 static int window_tile_rows(const WindowProb &p, int dh) { return dh * (p.dtype == DT_BF16 ? 2 : 4) > 256 ? 32 : 64; }
-// Two waves per 32 queries where the blocks of 128 are at most two per compute unit
-int window_key_groups(const WindowProb &p, int dh, int64_t blocks) { return window_tile_rows(p, dh) == 64 && blocks <= 512 ? 2 : 1; }
+// Two waves per 32 queries where the blocks of 128 do not give every compute unit one, in fp32 two, whose products take sixteen times as
+// long.  Step of 2 samples, bf16, heads of 64, window 128 / all earlier keys: 256 blocks 52 -> 48 / 88 -> 77 us, 512 blocks 70 -> 74 /
+// 171 -> 161; heads of 128, window 256: 256 blocks 85 -> 82, 512 blocks 99 -> 112; fp32: 128 blocks 75 -> 63, 512 blocks 182 -> 175.
+int window_key_groups(const WindowProb &p, int dh, int64_t blocks) {
+  return window_tile_rows(p, dh) == 64 && blocks <= (p.dtype == DT_BF16 ? 256 : 512) ? 2 : 1;
+}
 // whether the backward pass is one launch: its workgroups, one per compute unit, all run at once
 bool window_one_backward(int64_t workgroups) { return workgroups <= 256; }
 void window_plan_queries(WindowProb &p, int rows) {
@@ -1095,7 +1099,7 @@ void window_plan_queries(WindowProb &p, int rows) {
 // Cuts the key blocks of a launch (see WinUnit) into units, of which `slots` run at once: the first `whole` blocks stay in one piece,
 // the others and the blocks of the first tokens, which take several times as long, go in parts of part_steps steps, which fill the
 // gaps that whole blocks leave.  Of the pairs (whole, part_steps) the one with the least estimate, in steps: what a slot has to do, but
-// no less than the rounds of whole blocks, plus half a part of unevenness; a unit costs the time of some steps for its operands
+// no less than the rounds of whole blocks, plus half a part of unevenness (equal units: their rounds); a unit costs the time of some steps for its operands
 // and its result (4 us: about four steps of 64 x 128 pairs in bf16, half a one in fp32), a part its sums' way through memory, the
 // joining launch (5 us) the same for all.  one_round: no more units than slots, if there is such a pair (units = 0: there is none).
 void window_plan_parts(WindowProb &p, int dh, int slots, bool one_round) {
@@ -1110,7 +1114,8 @@ void window_plan_parts(WindowProb &p, int dh, int slots, bool one_round) {
   double best = 1e300;
   p.units = 0;
   for (int64_t whole = blocks;; whole = std::max<int64_t>(0, std::min(whole - 1, whole - slots / 8) / 8 * 8)) {
-    for (int64_t part = p.dtype == DT_BF16 ? 8 : 1; part < 2 * every + 8; part += part < 8 ? 1 : (part < 32 ? 4 : part / 8)) {
+    for (int64_t k = 0; k < 128; ++k) {      // even cuts of a regular block, and of one of the first tokens
+      const int64_t part = std::max<int64_t>(up(k < 64 ? regular : every, k % 64 + 1), p.dtype == DT_BF16 ? 8 : 1);
       const int64_t rest = blocks - whole, parts = up(regular, part), sink_parts = sb ? up(every, part) : 1;
       const int64_t split = (parts > 1 ? rest * parts : 0) + (sink_parts > 1 ? bg * sb * sink_parts : 0);
       const int64_t units = whole + rest * parts + bg * sb * sink_parts;
@@ -1118,7 +1123,10 @@ void window_plan_parts(WindowProb &p, int dh, int slots, bool one_round) {
       const double slot = (steps + start * (double)units) / slots;
       const double longest = std::max((double)(whole ? regular : 0), (double)std::min(part, std::max(rest ? regular : 0, sb ? every : 0))) + start;
       const double rounds = triangle ? longest : (double)up(whole, slots) * (regular + start);
-      const double t = std::max(std::max(slot, longest), rounds) + 0.5 * (split ? (double)part : 0.0) + (split ? join + sums * (double)split : 0.0);
+      const bool equal = !triangle && sb == 0 && (whole == 0 || rest == 0);      // (then it is so many rounds of the same unit)
+      const double t = (equal ? (double)up(units, slots) * ((double)(rest == 0 ? regular : std::min(part, regular)) + start)
+                              : std::max(std::max(slot, longest), rounds) + 0.5 * (split ? (double)part : 0.0)) +
+                       (split ? join + sums * (double)split : 0.0);
       if (t >= best || (one_round && units > slots)) continue;
       best = t;
       p.whole = (int32_t)whole;
