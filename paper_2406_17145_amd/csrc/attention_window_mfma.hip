@@ -356,7 +356,9 @@ __device__ __forceinline__ WinWave win_wave(const WindowProb &p, int q0, int len
 }
 
 // block of queries: key / value heads outermost, the query heads that share one innermost: workgroups that run together read the same
-// keys.  Where a causal block's work grows with its place, light and heavy blocks alternate, so that every XCD's share weighs the same
+// keys.  Where a causal block's work grows with its place, the heavier half comes first, from the heaviest on, and then the lighter one
+// from the lightest on: the two blocks that a compute unit gets of one run are as much work wherever it stands (2 x 2048 rows, 16 heads
+// of 64: forward 43.5 -> 41.3 us against light and heavy in turn)
 struct WinBlock {
   int b, h, g, r0;       // sample, query head, key / value head, first query
   bool first;            // of the query heads that share the key / value head
@@ -368,7 +370,8 @@ __device__ __forceinline__ WinBlock win_query_block(const WindowProb &p, int blk
   w.g = bg.r;
   w.h = bg.r * (int)p.by_group.d + hh.r;
   w.first = hh.r == 0;
-  w.r0 = (p.causal && !p.window ? ((k.r & 1) ? k.r >> 1 : (int)p.by_query_blocks.d - 1 - (k.r >> 1)) : k.r) * rows;
+  const int nb = (int)p.by_query_blocks.d, heavy = (nb + 1) >> 1;
+  w.r0 = (p.causal && !p.window ? (k.r < heavy ? nb - 1 - k.r : k.r - heavy) : k.r) * rows;
   return w;
 }
 
@@ -1098,44 +1101,58 @@ void window_plan_queries(WindowProb &p, int rows) {
 
 // Cuts the key blocks of a launch (see WinUnit) into units, of which `slots` run at once: the first `whole` blocks stay in one piece,
 // the others and the blocks of the first tokens, which take several times as long, go in parts of part_steps steps, which fill the
-// gaps that whole blocks leave.  Of the pairs (whole, part_steps) the one with the least estimate, in steps: what a slot has to do, but
-// no less than the rounds of whole blocks, plus half a part of unevenness (equal units: their rounds); a unit costs the time of some steps for its operands
-// and its result (4 us: about four steps of 64 x 128 pairs in bf16, half a one in fp32), a part its sums' way through memory, the
-// joining launch (5 us) the same for all.  one_round: no more units than slots, if there is such a pair (units = 0: there is none).
+// gaps that whole blocks leave.  Of the pairs (whole, part_steps) the one with the least estimate, in steps.  Units of one size take
+// their rounds; otherwise it is what a slot has to do, but no less than the rounds of whole blocks, plus half a part of unevenness.  A
+// unit costs the time of some steps for its operands and its result (4 us: about four steps of 64 x 128 pairs in bf16, half a
+// one in fp32), a part its sums' way through memory, the joining launch (5 us) the same for all.
+// one_round: no more units than slots, if there is such a pair (units = 0: there is none).
 void window_plan_parts(WindowProb &p, int dh, int slots, bool one_round) {
   const int64_t kt = window_tile_rows(p, dh), group = p.heads / p.kv_heads, seq = p.seq, nb = (seq + WIN_ROWS - 1) / WIN_ROWS;
   const int64_t win = p.window ? std::min<int64_t>(p.window, seq) : seq, bg = (int64_t)p.batch * p.kv_heads;
   const int64_t sb = p.window ? (std::min<int64_t>(p.sinks, seq) + WIN_ROWS - 1) / WIN_ROWS : 0;
-  auto tiles = [&](int64_t queries) { return std::min<int64_t>((std::min(queries, seq) + kt - 1) / kt + 1, (seq + kt - 1) / kt); };
+  auto up = [](int64_t v, int64_t by) { return (v + by - 1) / by; };
+  auto tiles = [&](int64_t queries) { return std::min<int64_t>(up(std::min(queries, seq), kt) + 1, up(seq, kt)); };
   const int64_t regular = group * tiles(WIN_ROWS - 1 + (p.causal ? win : 2 * win - 1)), every = group * tiles(seq), blocks = bg * (nb - sb);
   const bool triangle = p.causal && !p.window;       // half of the steps of a regular block, on average; the first blocks have most
-  auto up = [](int64_t v, int64_t by) { return (v + by - 1) / by; };
-  const double start = p.dtype == DT_BF16 ? 4.0 : 0.5, join = p.dtype == DT_BF16 ? 6.0 : 0.75, sums = p.dtype == DT_BF16 ? 0.00035 * dh : 0.00005 * dh;
+  const bool wide = p.dtype != DT_BF16;
+  const double start = wide ? 0.5 : 4.0, join = wide ? 0.75 : 6.0, sums = (wide ? 0.00005 : 0.00035) * dh;
+  const double steps = (double)blocks * regular * (triangle ? 0.5 : 1.0) + (double)(bg * sb * every);
   double best = 1e300;
   p.units = 0;
-  for (int64_t whole = blocks;; whole = std::max<int64_t>(0, std::min(whole - 1, whole - slots / 8) / 8 * 8)) {
-    for (int64_t k = 0; k < 128; ++k) {      // even cuts of a regular block, and of one of the first tokens
-      const int64_t part = std::max<int64_t>(up(k < 64 ? regular : every, k % 64 + 1), p.dtype == DT_BF16 ? 8 : 1);
-      const int64_t rest = blocks - whole, parts = up(regular, part), sink_parts = sb ? up(every, part) : 1;
-      const int64_t split = (parts > 1 ? rest * parts : 0) + (sink_parts > 1 ? bg * sb * sink_parts : 0);
-      const int64_t units = whole + rest * parts + bg * sb * sink_parts;
-      const double steps = (double)blocks * regular * (triangle ? 0.5 : 1.0) + (double)(bg * sb * every);
-      const double slot = (steps + start * (double)units) / slots;
-      const double longest = std::max((double)(whole ? regular : 0), (double)std::min(part, std::max(rest ? regular : 0, sb ? every : 0))) + start;
-      const double rounds = triangle ? longest : (double)up(whole, slots) * (regular + start);
-      const bool equal = !triangle && sb == 0 && (whole == 0 || rest == 0);      // (then it is so many rounds of the same unit)
-      const double t = (equal ? (double)up(units, slots) * ((double)(rest == 0 ? regular : std::min(part, regular)) + start)
-                              : std::max(std::max(slot, longest), rounds) + 0.5 * (split ? (double)part : 0.0)) +
-                       (split ? join + sums * (double)split : 0.0);
-      if (t >= best || (one_round && units > slots)) continue;
-      best = t;
-      p.whole = (int32_t)whole;
-      p.part_steps = (int32_t)part;
-      p.parts = (int32_t)parts;
-      p.sink_parts = (int32_t)sink_parts;
-      p.units = (int32_t)units;
-      p.rest = (int32_t)rest;
+  auto consider = [&](int64_t whole, int64_t part) {
+    const int64_t rest = blocks - whole, parts = up(regular, part), sink_parts = sb ? up(every, part) : 1;
+    const int64_t split = (parts > 1 ? rest * parts : 0) + (sink_parts > 1 ? bg * sb * sink_parts : 0);
+    const int64_t units = whole + rest * parts + bg * sb * sink_parts;
+    const double slot = (steps + start * (double)units) / slots;
+    const double longest = std::max(whole ? (double)regular : 0.0, (double)std::min(part, std::max(rest ? regular : 0, sb ? every : 0))) + start;
+    double t = std::max(slot, longest);
+    if (!triangle && sb == 0 && (whole == 0 || rest == 0)) {
+      t = (double)up(units, slots) * ((double)(rest == 0 ? regular : std::min(part, regular)) + start);
+    } else if (triangle && whole == 0) {      // parts that hold something, while their rounds are few
+      int64_t filled = 0;
+      for (int64_t c = 0; c < nb; ++c) filled += up(group * (tiles(seq) - c * WIN_ROWS / kt), part);
+      t = bg * filled <= 4 * slots ? (double)up(bg * filled, slots) * ((double)std::min(part, regular) + start) : t + 0.5 * (double)part;
+    } else {
+      if (!triangle) t = std::max(t, (double)up(whole, slots) * (regular + start));
+      if (split) t += 0.5 * (double)part;
     }
+    if (split) t += join + sums * (double)split;
+    if (t >= best || (one_round && units > slots)) return;
+    best = t;
+    p.whole = (int32_t)whole;
+    p.rest = (int32_t)rest;
+    p.part_steps = (int32_t)part;
+    p.parts = (int32_t)parts;
+    p.sink_parts = (int32_t)sink_parts;
+    p.units = (int32_t)units;
+  };
+  const int64_t least = wide ? 1 : 8;
+  for (int64_t whole = blocks;; whole = triangle ? 0 : std::max<int64_t>(0, std::min(whole - 1, whole - slots / 8) / 8 * 8)) {
+    for (int64_t k = 1; k <= 64; ++k) {
+      consider(whole, std::max(least, up(regular, k)));
+      if (sb) consider(whole, std::max(least, up(every, k)));
+    }
+    for (int64_t part = least; triangle && part <= 256; ++part) consider(whole, part);
     if (whole == 0) break;
   }
   p.sink_blocks = (int32_t)sb;
