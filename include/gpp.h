@@ -101,7 +101,8 @@ typedef enum {
                                (window == 0 or |i - j| < window or j < sinks).  in[1], optional: lengths input (i32, [b, 1], 0 to
                                S each); rows of a sample at and behind its length are padding: not read, output and
                                gradients zero.  out_features = heads*head_dim, S = seq_len.  The values of rows that are not
-                               padding have to be finite: a key's NaN or infinity may reach queries that do not see it */
+                               padding have to be finite: a key's NaN or infinity may reach queries that do not see it.
+                               A caller's tensor that either operator writes must not overlap one that it reads */
 } gpp_op_kind_t;
 
 /* GPP_OP_ROTARY: which columns of a head form pair i */
@@ -152,7 +153,7 @@ typedef struct {
   union {
     double eps;          /* LAYERNORM */
     double base;         /* ROTARY: base of the frequencies, above 0 */
-    double scale;        /* ATTENTION_WINDOW: factor of the scores; 0 = 1/sqrt(head_dim) */
+    double scale;        /* ATTENTION_WINDOW: factor of the scores, 1e-37 to 1e38; 0 = 1/sqrt(head_dim) */
   };
   double loss_scale;     /* LOSS_*: carries the 1/B normalisation of the whole mini-batch, so that
                             micro-batch gradients sum to the full-batch gradient */

@@ -682,6 +682,25 @@ static gpp_status_t run_steps_group(gpp_stage *st, const std::vector<Step> &step
   return GPP_OK;
 }
 
+// Tensors of the caller that sequence operators work on themselves (the copies in front of and behind other operators take any
+// address of whole elements): their accesses are 16 bytes wide
+static bool wide_misaligned(const void *p) { return ((uintptr_t)p & 15) != 0; }
+static gpp_status_t check_direct(const Plan &pl, bool backward, const void *const *ins, void *const *outs) {
+  for (size_t k = 0; k < pl.input_ops.size(); ++k) {
+    const Node &nd = pl.nodes[pl.input_ops[k]];
+    if (!backward && nd.read_direct && nd.d.dtype != DT_I32 && wide_misaligned(ins[k]))
+      return fail(GPP_ERR_INVALID_ARG, "input " + std::to_string(k) + " is not 16-byte aligned");
+    if (backward && nd.gin_direct && outs && wide_misaligned(outs[k]))
+      return fail(GPP_ERR_INVALID_ARG, "grad_inputs[" + std::to_string(k) + "] is not 16-byte aligned");
+  }
+  for (size_t k = 0; k < pl.output_ops.size(); ++k) {
+    const Node &nd = pl.nodes[pl.output_ops[k]];
+    if (nd.out_direct && (backward ? nd.wants_grad && wide_misaligned(ins[k]) : wide_misaligned(outs[k])))
+      return fail(GPP_ERR_INVALID_ARG, std::string(backward ? "grad_outputs[" : "outputs[") + std::to_string(k) + "] is not 16-byte aligned");
+  }
+  return GPP_OK;
+}
+
 extern "C" {
 
 gpp_status_t gpp_stage_forward(gpp_stage_t *st, int32_t slot, const void *const *inputs, void *const *outputs,
@@ -696,7 +715,9 @@ gpp_status_t gpp_stage_forward(gpp_stage_t *st, int32_t slot, const void *const 
   if (st->slot_busy[slot] == 2)
     return fail(GPP_ERR_ORDER, "slot " + std::to_string(slot) + " waits for gpp_stage_backward_weights (grouped weight gradients)");
   if (st->slot_busy[slot]) return fail(GPP_ERR_ORDER, "slot " + std::to_string(slot) + " still holds a micro-batch in flight");
-  gpp_status_t rc = run_steps(st, pl.fwd, slot, inputs, outputs, loss_out, 0, (hipStream_t)hip_stream);
+  gpp_status_t rc = check_direct(pl, false, inputs, outputs);
+  if (rc != GPP_OK) return rc;
+  rc = run_steps(st, pl.fwd, slot, inputs, outputs, loss_out, 0, (hipStream_t)hip_stream);
   if (rc != GPP_OK) return rc;
   st->slot_busy[slot] = 1;
   st->fifo.push_back(slot);
@@ -717,7 +738,9 @@ gpp_status_t gpp_stage_backward(gpp_stage_t *st, int32_t slot, const void *const
     for (size_t k = 0; k < pl.output_ops.size(); ++k)
       if (pl.nodes[pl.output_ops[k]].wants_grad && !grad_outputs[k]) return fail(GPP_ERR_INVALID_ARG, "grad_outputs[" + std::to_string(k) + "] is null");
   }
-  gpp_status_t rc = run_steps(st, pl.bwd, slot, grad_outputs, grad_inputs, nullptr, st->fresh ? 0 : 1, (hipStream_t)hip_stream);
+  gpp_status_t rc = check_direct(pl, true, grad_outputs, grad_inputs);
+  if (rc != GPP_OK) return rc;
+  rc = run_steps(st, pl.bwd, slot, grad_outputs, grad_inputs, nullptr, st->fresh ? 0 : 1, (hipStream_t)hip_stream);
   if (rc != GPP_OK) return rc;
   st->fresh = false;
   st->fifo.pop_front();

@@ -383,3 +383,40 @@ def test_a_pipeline_of_two_stages():
     assert keep is not None
     for x in st:
         x.close()
+
+
+@pytest.mark.parametrize("op", ["attention", "rotary"])
+def test_misaligned_tensors_are_refused(op):
+    """On the host, before anything is enqueued; the stage can be used afterwards."""
+    ops = S.attention_ops(1, 9, 2, 1, 16) if op == "attention" else S.rotary_ops(1, 9, 2, 16, (8,), rest=32)
+    batch, gout = S.draw(ops, 1, 16, {1: lambda r, s: r.integers(0, 99, s)})
+    st = B.Stage(ops, 1, {})
+    ins, g = st.stage_inputs(batch), st.to_device(len(ops) - 1, gout[len(ops) - 1])
+    outs, gin = st.alloc_outputs(), st.alloc_grad_inputs()
+    fw = [t.data_ptr() for t in ins], [outs[0].data_ptr()]
+    bw = [g.data_ptr()], [None if t is None else t.data_ptr() for t in gin]
+
+    def moved(ptrs):
+        return [ptrs[0] + 8] + ptrs[1:]
+
+    def refused(call, a, b):
+        with pytest.raises(B.GppError) as e:
+            call(a, b)
+        assert e.value.status == B.GPP_ERR_INVALID_ARG and "16-byte" in str(e.value)
+
+    def forward(a, b):
+        B.gpp_stage_forward(st.handle, 0, a, b, None, st.stream())
+
+    def backward(a, b):
+        B.gpp_stage_backward(st.handle, 0, a, b, st.stream())
+    refused(forward, moved(fw[0]), fw[1])
+    refused(forward, fw[0], moved(fw[1]))
+    forward(*fw)
+    refused(backward, moved(bw[0]), bw[1])
+    refused(backward, bw[0], moved(bw[1]))
+    backward(*bw)
+    torch.cuda.synchronize()
+    ref = S.oracle(ops, 1, batch, gout)
+    check("out", outs[0].float().cpu().numpy(), ref[0], bars("bf16", 9)[0])
+    check("grad", gin[0].float().cpu().numpy(), ref[1], bars("bf16", 9)[1])
+    st.close()
