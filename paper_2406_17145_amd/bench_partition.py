@@ -41,6 +41,14 @@ def op_costs(wl):
             s, d = op.get("seq_len", r), feat
             flops = 4.0 * 3.5 * s * s * d                    # forward + backward with recomputation
             bytes_ = 8 * r * d * e
+        elif k == "attention_window":
+            s, causal = op["seq_len"], op.get("causal", False)
+            near = min(op.get("window", 0) or s, s)
+            first = min(op.get("sinks", 0), s - near)
+            pairs = (s * near - near * (near - 1) / 2) * (1 if causal else 2) - (0 if causal else s)    # of a query and a key in its window
+            pairs += first * (s - near) - first * (first - 1) / 2                                      # and a first token in front of it
+            flops = 4.0 * 3.5 * pairs * feat
+            bytes_ = 4 * r * feat * (1 + 2 * op["kv_heads"] / op["heads"]) * e + 4 * r * feat * e
         elif k == "embedding_bag_sum":
             bytes_ = 3 * op["bag_size"] * feat * 4
             params = op["num_rows"] * feat

@@ -206,6 +206,8 @@ def build_desc(ops, micro_batch, slots=1, flags=0, param_ptrs=None, grad_ptrs=No
             d.grad[k] = (grad_ptrs or {}).get(i, [None, None])[k]
         # (these operators' own names for fields of the structure, see the unions of gpp_op_desc_t)
         if op["kind"] == "rotary":
+            if len(op["axis_pairs"]) > 4:
+                raise ValueError("rotary: at most four axes")
             d.in_features, d.eps = op["head_dim"], op["base"]
             d.act, d.has_bias = PAIRINGS[op.get("pairing", "halves")], LADDERS[op.get("ladder", "shared")]
             d.num_rows = int.from_bytes(struct.pack("<4h", *(list(op["axis_pairs"]) + [0] * 4)[:4]), "little", signed=True)

@@ -1079,7 +1079,7 @@ int window_mfma_dh(const WindowProb &p) {
   if (p.dtype == DT_I32 || p.out_dtype != p.dtype || p.dh > 128 || p.dh % epc) return 0;
   if ((p.ld_qkv | p.ld_out | p.ld_o | p.ld_dout | p.ld_ext) % epc) return 0;
   if (((uintptr_t)p.qkv | (uintptr_t)p.out | (uintptr_t)p.o | (uintptr_t)p.dout) & 15) return 0;
-  if ((p.ld_qkv | p.ld_dout) >= (1ll << 24)) return 0;        // a tile's offsets stay far inside 32 bits
+  if ((p.ld_qkv | p.ld_o | p.ld_dout) >= (1ll << 22)) return 0;        // a tile's offsets stay far inside 32 bits
   return p.dh <= 32 ? 32 : (p.dh <= 64 ? 64 : (p.dh <= 96 ? 96 : 128));
 }
 static int window_tile_rows(const WindowProb &p, int dh) { return dh * (p.dtype == DT_BF16 ? 2 : 4) > 256 ? 32 : 64; }

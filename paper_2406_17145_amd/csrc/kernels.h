@@ -144,7 +144,7 @@ struct WindowProb {
   GPP_G void *o;           // bwd: O (forward output)
   const GPP_G void *dout;  // bwd: dO
   GPP_G float *lse;        // [b*heads, S] log2 of the sum of 2^(scores in base 2); bwd reads it
-  GPP_G float *delta;      // bwd: [b*heads, S] rowsum(dO * O), written with dQ
+  GPP_G float *delta;      // bwd: [b*heads, S] rowsum(dO * O), written with dQ (negative by the matrix-core kernels)
   const GPP_G int32_t *lengths;   // [b], or null with ext_len < 0: all S
   GPP_G int32_t *lengths_keep;    // fwd, or null: the lengths are copied here for the backward pass
   GPP_G void *qkv_keep;    // fwd, or null: the rows behind ext_qkv are copied here for the backward pass

@@ -150,6 +150,7 @@ gpp_status_t Plan::analyse(const gpp_stage_desc_t *desc) {
         }
         if (axes == 0) FAIL(GPP_ERR_INVALID_ARG, "rotary: no axis");
         if (2 * pairs > d.head_dim) FAIL(GPP_ERR_SHAPE, "rotary: more pairs than a head has columns for");
+        if (nd.rows / rotary_rows_per_block(nd.rows, (int)std::min<int64_t>(pairs, rotary_max_pairs())) > (1 << 23)) FAIL(GPP_ERR_UNSUPPORTED, "rotary: too many rows for this build");
         if (pairs > rotary_max_pairs()) FAIL(GPP_ERR_UNSUPPORTED, "rotary: too many pairs for this build");
         if (!(d.base > 0) || !std::isfinite(d.base)) FAIL(GPP_ERR_INVALID_ARG, "rotary: base must be positive");
         if (d.pairing != GPP_PAIR_HALVES && d.pairing != GPP_PAIR_NEIGHBOURS) FAIL(GPP_ERR_INVALID_ARG, "rotary: bad pairing");
@@ -171,7 +172,9 @@ gpp_status_t Plan::analyse(const gpp_stage_desc_t *desc) {
         if (nd.rows * (int64_t)d.heads > (1 << 25)) FAIL(GPP_ERR_UNSUPPORTED, "windowed attention: too many rows and heads");
         if (d.window < 0 || d.sinks < 0) FAIL(GPP_ERR_INVALID_ARG, "windowed attention: window and sinks must not be negative");
         if (d.causal != 0 && d.causal != 1) FAIL(GPP_ERR_INVALID_ARG, "windowed attention: causal is 0 or 1");
-        if (!(d.scale >= 0) || !std::isfinite((float)d.scale)) FAIL(GPP_ERR_INVALID_ARG, "windowed attention: scale must be positive (0: 1/sqrt(head_dim))");
+        // (as the kernels hold it: in fp32, times log2 e)
+        if (!(d.scale >= 0) || (float)d.scale > 1e38f || (d.scale > 0 && (float)d.scale < 1e-37f))
+          FAIL(GPP_ERR_INVALID_ARG, "windowed attention: scale must be between 1e-37 and 1e38 (0: 1/sqrt(head_dim))");
         if (!is_float(d.dtype) || !is_float(in(0).d.dtype)) FAIL(GPP_ERR_UNSUPPORTED, "windowed attention: float dtypes only");
         if (nd.in.size() == 2) {
           if (in(1).d.kind != GPP_OP_INPUT || in(1).d.dtype != GPP_I32) FAIL(GPP_ERR_BAD_GRAPH, "windowed attention: lengths must be an i32 input");

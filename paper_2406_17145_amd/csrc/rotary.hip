@@ -16,13 +16,14 @@ static_assert(ROT_MAX_PAIRS <= ROT_LDS, "the angles of a row fit");
 
 int rotary_max_pairs() { return ROT_MAX_PAIRS; }
 
-// Elements that a lane moves at once: 16 bytes where a pair's two columns (halves), a head and a row allow it, 4 bytes of bf16
-// neighbours or 8 bytes of fp32 ones where only that, single elements otherwise.
+// Elements that a lane moves at once: 16 bytes where a pair's two columns (halves), a head, a row and the address allow it, or 8
+// or 4 where only that, single elements otherwise.
 int rotary_vec(const RotaryProb &p) {
   const int whole = p.dtype == DT_BF16 ? 8 : 4;
   for (int v = whole; v > 1; v >>= 1) {
     const int64_t unit = p.neighbours ? 2 * p.pairs : p.pairs;      // columns whose partners lie beside them
-    if (unit % v == 0 && p.dh % v == 0 && p.cols % v == 0 && p.ld_x % v == 0 && p.ld_y % v == 0) return v;
+    const bool aligned = (((uintptr_t)p.x | (uintptr_t)p.y) & (v * (p.dtype == DT_BF16 ? 2 : 4) - 1)) == 0;
+    if (aligned && unit % v == 0 && p.dh % v == 0 && p.cols % v == 0 && p.ld_x % v == 0 && p.ld_y % v == 0) return v;
   }
   return 1;
 }

@@ -168,6 +168,18 @@ def test_rotary_refusals(lib):
     assert _status(S.rotary_ops(4, 4, 1, 2048, (1000,))) == B.GPP_ERR_UNSUPPORTED
 
 
+def test_refusals_at_the_ends_of_ranges(lib):
+    ops = S.attention_ops(4, 16, 4, 2, 64)
+    for scale in (1e-50, 1e-40, 2e38):          # fp32 holds no such factor, or no product with log2 e
+        assert _status(_changed(ops, 1, scale=scale)) == B.GPP_ERR_INVALID_ARG
+    for scale in (1e-30, 1e30):
+        d, keep = B.build_desc(_changed(ops, 1, scale=scale), 4)
+        assert B.gpp_stage_workspace_bytes(d) > 0
+    with pytest.raises(ValueError):
+        B.build_desc(S.rotary_ops(4, 16, 6, 64, (1, 1, 1, 1, 1)), 4)
+    assert _status(S.rotary_ops(1, 1 << 29, 1, 2, (1,)), 1) == B.GPP_ERR_UNSUPPORTED      # more workgroups than a launch has
+
+
 def _launches(ops, b):
     d, keep = B.build_desc(ops, b)
     # (without loss operators the loss sum writes a zero where the caller asks for one)
@@ -198,3 +210,13 @@ def test_a_layer_in_front_of_a_rotary_shares_its_buffers(lib):
         d, keep = B.build_desc(wl.ops, wl.micro_batch)
         size.append(B.gpp_stage_workspace_bytes(d))
     assert size[1] - size[0] >= 3 * 32 * 384 * 2        # value, gradient, stashed derivative of [32, 384]
+
+
+def test_partition_costs_count_the_visible_pairs():
+    from types import SimpleNamespace
+    from paper_2406_17145_amd import bench_partition as P
+    for seq, window, sinks, causal in [(2048, 0, 0, True), (2048, 0, 0, False), (2048, 100, 30, True), (2048, 100, 0, False), (2048, 2048, 9, True)]:
+        ops = S.attention_ops(1, seq, 8, 2, 128, window=window, sinks=sinks, causal=causal)
+        _, t, _, _ = P.op_costs(SimpleNamespace(ops=ops, micro_batch=1))
+        seen = O.window_mask(seq, ops[1]).sum()
+        assert abs(t[1] - max(4 * 3.5 * seen * 1024 / P.MFMA_RATE, seq * 1024 * 2 * (4 * 1.5 + 4) / P.MEM_RATE)) <= 1e-12 * t[1]
