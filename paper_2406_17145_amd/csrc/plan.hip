@@ -811,6 +811,14 @@ struct Emitter {
           one = false;
           plan_keys();
         }
+        if (dh && backward && !one) {
+          int64_t units = 0, joins = 0;
+          for (auto &a : now) {
+            units += a.units;
+            joins += window_join_blocks(a, dh);
+          }
+          one = joins == 0 && window_beside(blocks128, units);
+        }
         for (auto &a : now) window_plan_queries(a, one ? 128 : 128 / groups);
         auto queries = [&](const WindowProb &a) { return dh ? a.query_units : window_blocks(a.batch, a.heads, a.seq); };
         if (!backward) {

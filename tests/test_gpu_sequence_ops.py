@@ -113,6 +113,13 @@ def test_window_long(window, sinks):
     run_attention(b=1, seq=2500, heads=2, kv=1, dh=64, window=window, sinks=sinks, causal=False)
 
 
+@pytest.mark.parametrize("dh", [32, 64, 128])
+@pytest.mark.parametrize("values", [None, [128, 0, 77, 1, 100, 128, 33, 64]])
+def test_window_short_samples(dh, values):
+    """Few blocks of keys that many query heads share, beside the blocks of queries."""
+    run_attention(b=8, seq=128, heads=24, kv=3, dh=dh, window=70, sinks=2, causal=True, values=values)
+
+
 @pytest.mark.parametrize("b,heads,kv,causal", [(1, 2, 1, True), (3, 4, 4, False)])
 def test_window_many_first_tokens(b, heads, kv, causal):
     """First tokens over several blocks of keys, whose work is cut into parts, with samples that end inside them."""
@@ -419,4 +426,45 @@ def test_misaligned_tensors_are_refused(op):
     ref = S.oracle(ops, 1, batch, gout)
     check("out", outs[0].float().cpu().numpy(), ref[0], bars("bf16", 9)[0])
     check("grad", gin[0].float().cpu().numpy(), ref[1], bars("bf16", 9)[1])
+    st.close()
+
+
+def test_rows_beyond_32_bits():
+    """[2 x 2^18, 6144]: offsets of the second sample pass 2^31 elements and 2^32 bytes.  The last queries and keys against a dense
+    calculation in fp64 over the rows that they can see."""
+    s, heads, kv, dh, window, sinks, tail = 1 << 18, 32, 8, 128, 100, 3, 200
+    ops = S.attention_ops(2, s, heads, kv, dh, window=window, sinks=sinks, causal=True)
+    st = B.Stage(ops, 2, {})
+    gen = torch.Generator(device="cuda").manual_seed(17)
+    x = torch.empty(2 * s, (heads + 2 * kv) * dh, dtype=torch.bfloat16, device="cuda").normal_(generator=gen)
+    g = torch.empty(2 * s, heads * dh, dtype=torch.bfloat16, device="cuda").normal_(generator=gen)
+    out, gx = torch.empty_like(g), torch.empty_like(x)
+    B.gpp_stage_forward(st.handle, 0, [x.data_ptr()], [out.data_ptr()], None, st.stream())
+    B.gpp_stage_backward(st.handle, 0, [g.data_ptr()], [gx.data_ptr()], st.stream())
+    torch.cuda.synchronize()
+    rows = torch.cat([torch.arange(sinks), torch.arange(s - tail - window, s)])
+    part = x[(s + rows).cuda()].cpu().double().requires_grad_()
+    r = part.reshape(len(rows), heads + 2 * kv, dh).transpose(0, 1)
+    back = rows[-tail:, None] - rows[None, :]
+    seen = (back >= 0) & ((back < window) | (rows[None, :] < sinks))
+    k, v = (r[a:a + kv].repeat_interleave(heads // kv, 0) for a in (heads, heads + kv))
+    p = ((r[:heads, -tail:] @ k.transpose(1, 2)) * dh ** -0.5).masked_fill(~seen, -float("inf")).softmax(-1)
+    ref = (p @ v).transpose(0, 1).reshape(tail, heads * dh)
+    (ref * g[-tail:].cpu().double()).sum().backward()
+    check("out", out[-tail:].float().cpu().numpy(), ref.detach().numpy(), bars("bf16", window)[0])
+    check("grad", gx[-tail:].float().cpu().numpy(), part.grad[-tail:].numpy(), bars("bf16", window)[1])
+    st.close()
+    del st, out, gx, g
+    ops = S.rotary_ops(2, s, heads + kv, dh, (64,), rest=kv * dh)
+    st = B.Stage(ops, 2, {})
+    pos = torch.arange(2 * s, dtype=torch.int32, device="cuda").reshape(-1, 1)
+    y = torch.empty_like(x)
+    B.gpp_stage_forward(st.handle, 0, [x.data_ptr(), pos.data_ptr()], [y.data_ptr()], None, st.stream())
+    torch.cuda.synchronize()
+    a = x[-tail:].cpu().double()
+    t = pos[-tail:].cpu().double() * 10000.0 ** (-torch.arange(64).double() / 64)
+    cos, sin = (f(t)[:, None] for f in (torch.cos, torch.sin))
+    q = a[:, :(heads + kv) * dh].reshape(tail, heads + kv, 2, 64)
+    turned = torch.stack([q[:, :, 0] * cos - q[:, :, 1] * sin, q[:, :, 0] * sin + q[:, :, 1] * cos], 2).reshape(tail, -1)
+    check("rotary", y[-tail:].float().cpu().numpy(), torch.cat([turned, a[:, (heads + kv) * dh:]], 1).numpy(), S.HALF_STEP["bf16"])
     st.close()
