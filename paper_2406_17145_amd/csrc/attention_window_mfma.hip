@@ -699,15 +699,6 @@ __device__ __forceinline__ void win_dq_body(const WindowProb &p, const ExtPtrs &
     win_store_rows<T, DH>(lds, qg, dq, p.scale, q0, len, p.seq, p.dh, dqkv, row0, p.ld_out, nullptr, 0, (int64_t)w.h * p.dh);
 }
 
-template <typename T, int DH, int KG>
-__global__ __launch_bounds__(256, 2) void k_window_dq_mfma(const WindowProb *__restrict__ probs, int n, ExtPtrs ext) {
-  __shared__ __attribute__((aligned(16))) unsigned char lds[WinQueryCfg<T, DH, 4, KG>::LDS];
-  const int pi = find_prob(probs, n, blockIdx.x);
-  const WindowProb p = probs[pi];
-  win_fetch(p);
-  win_dq_body<T, DH, 4, KG, true>(p, ext, blockIdx.x - p.blk_begin, lds);
-}
-
 // ======================================================================= backward: dK, dV
 // The steps of a block of keys are the tiles of queries that see one of them, for every query head that shares the keys, head by
 // head.  A block's steps go to one workgroup, or `parts` of at most `part_steps` to several, whose fp32 sums k_window_join adds in
@@ -1032,15 +1023,13 @@ __global__ __launch_bounds__((WinKeyCfg<T, DH, true>::NW * 64), (DH * sizeof(T) 
 
 // The sums of a split block's parts, in order: four columns of a key per thread, DH / 4 workgroups per block
 template <typename T, int DH>
-__global__ __launch_bounds__(256) void k_window_join(const WindowProb *__restrict__ probs, int n, ExtPtrs ext) {
+__device__ __forceinline__ void win_join_body(const WindowProb &p, const ExtPtrs &ext, int local) {
   typedef WinTile<T, DH> C;
-  const int pi = find_prob(probs, n, blockIdx.x);
-  const WindowProb p = probs[pi];
   GPP_G T *dqkv = (GPP_G T *)(p.ext_out >= 0 ? ext.p[p.ext_out] : p.out);
   if (!dqkv) return;
   const int rest = p.rest;
   const int regular = p.parts > 1 ? rest : 0;                     // split blocks that hold no first token
-  const int blk = (blockIdx.x - p.blk_begin) / (DH / 4), piece = (blockIdx.x - p.blk_begin) % (DH / 4);
+  const int blk = local / (DH / 4), piece = local % (DH / 4);
   const WinUnit w = win_unit(p, p.whole + (blk < regular ? blk * p.parts : rest * p.parts + (blk - regular) * p.sink_parts));
   const int first = w.slot, len = window_length(p, w.b);
   const int parts = (win_steps<C::KT>(p, w.c0, len).n + p.part_steps - 1) / p.part_steps;
@@ -1072,6 +1061,25 @@ __global__ __launch_bounds__(256) void k_window_join(const WindowProb *__restric
   }
 }
 
+template <typename T, int DH>
+__global__ __launch_bounds__(256) void k_window_join(const WindowProb *__restrict__ probs, int n, ExtPtrs ext) {
+  const int pi = find_prob(probs, n, blockIdx.x);
+  const WindowProb p = probs[pi];
+  win_join_body<T, DH>(p, ext, blockIdx.x - p.blk_begin);
+}
+
+// (and, where dK and dV went first, the joining of their parts)
+template <typename T, int DH, int KG>
+__global__ __launch_bounds__(256, 2) void k_window_dq_mfma(const WindowProb *__restrict__ probs, int n, ExtPtrs ext) {
+  __shared__ __attribute__((aligned(16))) unsigned char lds[WinQueryCfg<T, DH, 4, KG>::LDS];
+  const int pi = find_prob(probs, n, blockIdx.x);
+  const WindowProb p = probs[pi];
+  win_fetch(p);
+  const int local = blockIdx.x - p.blk_begin;
+  if (local < p.query_units) win_dq_body<T, DH, 4, KG, true>(p, ext, local, lds);
+  else win_join_body<T, DH>(p, ext, local - p.query_units);
+}
+
 // ---- host ------------------------------------------------------------------------------------------------
 // template head dimension of a record, or 0: the row-parallel kernels
 int window_mfma_dh(const WindowProb &p) {
@@ -1096,6 +1104,10 @@ bool window_one_backward(int64_t workgroups) { return workgroups <= 256; }
 // of 128 51.1 -> 42.1, over 16 30.2 -> 26.2; as many units as compute units (over 32) 45.7 -> 48.4 with heads of 128; 512 blocks of
 // queries 40.8 -> 39.0, 1024 of them 64.7 -> 68.9.
 bool window_beside(int64_t query_blocks, int64_t key_units) { return query_blocks <= 512 && key_units <= 128; }
+// Whether dK and dV, where they are split, go in front of dQ and form their own deltas: the joining of their parts is then in dQ's launch.
+// What the deltas cost grows with the steps and with the rows.  Step of 4 x 512, window 128, bf16, 16 heads over 4, 256 blocks: heads of
+// 64 48.1 -> 45.5 us, of 128 69.9 -> 73.8; 2 x 2048, window 512, heads of 64, 512 blocks: 84.7 -> 85.3; fp32 the same either way.
+bool window_keys_first(int dtype, int dh, int64_t query_blocks) { return dtype == DT_BF16 && dh <= 64 && query_blocks <= 256; }
 void window_plan_queries(WindowProb &p, int rows) {
   p.by_group = fast_div(p.heads / p.kv_heads);
   p.by_kv_heads = fast_div(p.kv_heads);

@@ -811,8 +811,9 @@ struct Emitter {
           one = false;
           plan_keys();
         }
+        int64_t joins = 0;
         if (dh && backward && !one) {
-          int64_t units = 0, joins = 0;
+          int64_t units = 0;
           for (auto &a : now) {
             units += a.units;
             joins += window_join_blocks(a, dh);
@@ -838,6 +839,11 @@ struct Emitter {
         if (one) {
           step(K_WINDOW_BWD, now, dt, dh, 1, [&](const WindowProb &a) { return a.units + a.query_units; });
           step(K_WINDOW_JOIN, now, dt, dh, 1, [&](const WindowProb &a) { return window_join_blocks(a, dh); });
+          continue;
+        }
+        if (joins > 0 && window_keys_first(dt, dh, blocks128)) {
+          step(K_WINDOW_BWD, now, dt, dh, 1, [&](const WindowProb &a) { return a.units; });
+          step(K_WINDOW_DQ, now, dt, dh, groups, [&](const WindowProb &a) { return a.query_units + window_join_blocks(a, dh); });
           continue;
         }
         step(K_WINDOW_DQ, now, dt, dh, groups, queries);
