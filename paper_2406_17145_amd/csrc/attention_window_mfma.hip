@@ -1163,7 +1163,7 @@ void window_plan_parts(WindowProb &p, int dh, int slots, bool one_round) {
     p.sink_parts = (int32_t)sink_parts;
     p.units = (int32_t)units;
   };
-  const int64_t least = wide ? 1 : 8;
+  const int64_t least = wide ? 1 : 2;
   for (int64_t whole = blocks;; whole = triangle ? 0 : std::max<int64_t>(0, std::min(whole - 1, whole - slots / 8) / 8 * 8)) {
     for (int64_t k = 1; k <= 64; ++k) {
       consider(whole, std::max(least, up(regular, k)));
