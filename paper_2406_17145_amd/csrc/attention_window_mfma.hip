@@ -497,12 +497,6 @@ __global__ __launch_bounds__(256, 2) void k_window_fwd_mfma(const WindowProb *__
 #pragma unroll
   for (int d = 0; d < C::DB; ++d) o[d] = win_zero();
   float m = -INFINITY, l = 0.0f;     // running maximum (base 2, the same in a lane and its partner) and sum (in fp32 of this lane's share)
-  // Narrow heads keep the vector unit busier than the matrix cores: there the probabilities are summed as a product with a row of ones
-  constexpr bool SUM_MMA = sizeof(T) == 2 && DH <= 64;
-  f32x16 ls = win_zero();
-  typename F::type ones;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) ones[e] = (decltype(+ones[0]))1.0f;
 
   // this wave's keys of a tile, N times 32
   auto part = [&](const unsigned char *tk, const unsigned char *tv, int k0, bool masked) {
@@ -534,8 +528,7 @@ __global__ __launch_bounds__(256, 2) void k_window_fwd_mfma(const WindowProb *__
     // rescaling of the output
     if (__ballot(m_tile > m + 8.0f) != 0ull) {
       const float m_new = fmaxf(m, m_tile), alpha = __builtin_amdgcn_exp2f(m - (m_new == -INFINITY ? 0.0f : m_new));
-      if (SUM_MMA) ls[0] *= alpha;      // (every row of the product is the same sum: one of them is kept)
-      else l *= alpha;
+      l *= alpha;
 #pragma unroll
       for (int d = 0; d < C::DB; ++d)
 #pragma unroll
@@ -548,12 +541,11 @@ __global__ __launch_bounds__(256, 2) void k_window_fwd_mfma(const WindowProb *__
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         st[i][r] = __builtin_amdgcn_exp2f(fmaf(st[i][r], scale2, -ref));
-        if (!SUM_MMA) l += st[i][r];
+        l += st[i][r];
       }
 #pragma unroll
     for (int c = 0; c < 2 * N; ++c) {
       const typename F::type pf = F::pack(st[c >> 1], c & 1);
-      if (SUM_MMA) ls = F::mma(ones, pf, ls);
 #pragma unroll
       for (int d = 0; d < C::DB; ++d) o[d] = F::mma(win_col_frag<T, DH>(at, tv, 16 * c, d), pf, o[d]);
     }
@@ -567,7 +559,7 @@ __global__ __launch_bounds__(256, 2) void k_window_fwd_mfma(const WindowProb *__
   WinKeep<T, DH, ROWS> keep;
   if (p.qkv_keep) keep.load(p, qkv, w, row0);
   __syncthreads();
-  l = SUM_MMA ? ls[0] : win_half_sum(l);
+  l = win_half_sum(l);
   if constexpr (KG == 2) {      // the second half's output, sum and maximum to the first half's waves
     float *join = (float *)lds + qg * 32 * (DH + 2) + lane;
     if (kg == 1) {
