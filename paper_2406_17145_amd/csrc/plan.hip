@@ -1461,14 +1461,14 @@ void Emitter::forward() {
           const Node &x = N[nd.in[0]], &q = N[nd.in[1]];
           RotaryProb r = rotary_record(nd, false);
           if (x.read_direct) {
-            r.ext_x = x.input_index;
+            r.ext_x = ext_read(x.input_index);
             r.ld_x = x.feat;
           } else {
             r.x = ptr(x.val);
             r.ld_x = x.val.ld;
           }
           if (nd.out_direct) {
-            r.ext_y = EXT_HALF + nd.output_index;
+            r.ext_y = ext_written(nd.output_index);
             r.ld_y = nd.feat;
           } else {
             r.y = ptr(nd.val);
@@ -1477,7 +1477,7 @@ void Emitter::forward() {
           r.in_place = nd.in_place;
           r.pos = (const int32_t *)ptr(q.val);
           if (q.read_direct) {
-            r.ext_pos = q.input_index;
+            r.ext_pos = ext_read(q.input_index);
             if (keeps(q, i)) r.pos_keep = (int32_t *)ptr(q.val);
           }
           rotaries.push_back(r);
@@ -1487,7 +1487,7 @@ void Emitter::forward() {
           const Node &x = N[nd.in[0]];
           WindowProb a = window_record(nd);
           if (x.read_direct) {
-            a.ext_qkv = x.input_index;
+            a.ext_qkv = ext_read(x.input_index);
             a.ld_qkv = x.feat;
             if (keeps(x, i)) {
               a.qkv_keep = ptr(x.val);
@@ -1500,14 +1500,14 @@ void Emitter::forward() {
           a.out = ptr(nd.val);
           a.ld_out = nd.val.ld;
           if (nd.out_direct) {
-            a.ext_out = EXT_HALF + nd.output_index;
+            a.ext_out = ext_written(nd.output_index);
             a.ld_ext = nd.feat;
           }
           a.lse = (float *)ptr(nd.stat0);
           if (nd.in.size() == 2) {
             const Node &q = N[nd.in[1]];
             if (q.read_direct) {
-              a.ext_len = q.input_index;
+              a.ext_len = ext_read(q.input_index);
               if (keeps(q, i)) a.lengths_keep = (int32_t *)ptr(q.val);
             }
           }
@@ -2113,7 +2113,7 @@ void Emitter::backward() {
           RotaryProb r = rotary_record(nd, true);
           r.pos = (const int32_t *)ptr(N[nd.in[1]].val);
           if (nd.out_direct) {
-            r.ext_x = nd.output_index;
+            r.ext_x = ext_read(nd.output_index);
             r.ld_x = nd.feat;
           } else {
             r.x = ptr(nd.gout);
@@ -2124,7 +2124,7 @@ void Emitter::backward() {
             r.y = ptr(nd.gout);
             r.ld_y = nd.gout.ld;
           } else if (x.gin_direct) {
-            r.ext_y = EXT_HALF + x.input_index;
+            r.ext_y = ext_written(x.input_index);
             r.ld_y = x.feat;
             gstate[nd.in[0]] = G_WRITTEN;
           } else {
@@ -2142,7 +2142,7 @@ void Emitter::backward() {
           a.qkv = ptr(x.val);
           a.ld_qkv = x.val.ld;
           if (x.gin_direct) {
-            a.ext_out = EXT_HALF + x.input_index;
+            a.ext_out = ext_written(x.input_index);
             a.ld_out = x.feat;
             a.grad_dtype = x.gdtype;
             gstate[nd.in[0]] = G_WRITTEN;
@@ -2153,7 +2153,7 @@ void Emitter::backward() {
             a.grad_dtype = tg.dst.dtype;
           }
           if (nd.out_direct) {
-            a.ext_dout = nd.output_index;
+            a.ext_dout = ext_read(nd.output_index);
             a.ld_dout = nd.feat;
           } else {
             a.dout = ptr(nd.gout);

@@ -472,8 +472,8 @@ static gpp_status_t run_steps(gpp_stage *st, const std::vector<Step> &steps, int
     if (sp.ext_kind == EXT_BOTH) {
       const int n_in = (int)pl.input_ops.size(), n_out = (int)pl.output_ops.size();
       for (int k = 0; k < EXT_HALF; ++k) {
-        if (k < (is_bwd ? n_out : n_in)) ext.p[k] = ext_in ? (void *)ext_in[k] : nullptr;
-        if (k < (is_bwd ? n_in : n_out)) ext.p[EXT_HALF + k] = ext_out ? ext_out[k] : nullptr;
+        if (k < (is_bwd ? n_out : n_in)) ext.p[ext_read(k)] = ext_in ? (void *)ext_in[k] : nullptr;
+        if (k < (is_bwd ? n_in : n_out)) ext.p[ext_written(k)] = ext_out ? ext_out[k] : nullptr;
       }
     } else if (sp.ext_kind != EXT_NONE) {
       const bool in_side = sp.ext_kind == EXT_INPUTS || sp.ext_kind == EXT_GRAD_OUTPUTS;
