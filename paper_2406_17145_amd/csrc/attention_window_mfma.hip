@@ -13,8 +13,17 @@
 //   forward      S^T = K Q^T              O^T  += V^T P^T
 //   backward dQ  S^T = K Q^T, dP^T = V dO^T,  dQ^T += K^T dS^T
 //   backward dKV S   = Q K^T, dP   = dO V^T,  dV += P^T dO,  dK += dS^T Q
-// P and dS enter the second products in the storage type, as operands of the matrix cores; all sums are fp32.  No atomics: dQ has
-// its own kernel, and sums over a long run of queries that are split over workgroups meet in a fixed order.
+// P and dS enter the second products in the storage type, as operands of the matrix cores; all sums are fp32.  In bf16 the gradients are
+// then off by 0.0024 (l2-relative), where rounding nothing but the results costs 0.0017; by up to 0.0031 in dQ and dK of samples of a few
+// tokens, where the rounding of O in rowsum(dO * O) weighs more.  No atomics: dQ has its own kernel, and sums over a long run of
+// queries that are split over workgroups meet in a fixed order.
+//
+// What bounds it.  Long rows: matrix cores and vector unit (exponentials, masks, conversions) of a SIMD's two waves are busy half of the
+// time each, and the clock falls under the load.  1 x 16384, window 4096, causal, 16 heads of 128 over 2, bf16: forward 573 us
+// (0.84 PFLOP/s of visible pairs, matrix cores busy 52 %), dQ 758 (0.95, 58 %), dK and dV 1016 - 1091 (0.9, 55 %), joining 12.  Heads of
+// 64: twice the vector work per product; 2 x 8192, window 1024, causal, 16 heads over 4: a step of 416 us, 0.70 PFLOP/s where
+// heads of 128 reach 0.95.  Short rows: a wave's chain through a tile, some 2000 cycles, between a launch's first loads and last stores; 4 x 512, window 128, 16 heads of
+// 64 over 4: forward 14 us, dK and dV 21, dQ and the joining 14.
 #include <algorithm>
 
 #include "gemm_direct.h"
@@ -464,6 +473,8 @@ __device__ __forceinline__ void win_stream_keys(const WinRange &tiles, int nt, W
 }
 
 // ======================================================================= forward
+// A workgroup's queries share the tiles of K and V; the softmax's running maximum and sum are of a lane's query, whose other 16 keys of 32
+// the partner lane holds.
 template <typename T, int DH, int KG>
 __global__ __launch_bounds__(256, 2) void k_window_fwd_mfma(const WindowProb *__restrict__ probs, int n, ExtPtrs ext, StageFlags *flags) {
   typedef WinTile<T, DH> C;
@@ -1013,7 +1024,8 @@ __global__ __launch_bounds__((WinKeyCfg<T, DH, true>::NW * 64), (DH * sizeof(T) 
   else win_dq_body<T, DH, K::NW, WinTile<T, DH>::SUB, false>(p, ext, local - p.units, lds);
 }
 
-// The sums of a split block's parts, in order: four columns of a key per thread, DH / 4 workgroups per block
+// The sums of a split block's parts, in order: four columns of a key per thread, DH / 4 workgroups per block (bound by memory; 12 us for
+// 1 x 16384, window 4096, 2 key / value heads of 128: a few MB, most of it a launch and one trip to memory)
 template <typename T, int DH>
 __device__ __forceinline__ void win_join_body(const WindowProb &p, const ExtPtrs &ext, int local) {
   typedef WinTile<T, DH> C;

