@@ -102,6 +102,7 @@ typedef enum {
                                S each); rows of a sample at and behind its length are padding: not read, output and
                                gradients zero.  out_features = heads*head_dim, S = seq_len.  The values of rows that are not
                                padding have to be finite: a key's NaN or infinity may reach queries that do not see it.
+                               head_dim up to 256, rows * heads up to 2^25, samples * heads up to 2^23.
                                A caller's tensor that either operator writes must not overlap one that it reads */
 } gpp_op_kind_t;
 

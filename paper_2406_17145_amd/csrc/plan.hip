@@ -169,7 +169,10 @@ gpp_status_t Plan::analyse(const gpp_stage_desc_t *desc) {
         if (d.seq_len <= 0 || nd.rows != micro_batch * d.seq_len) FAIL(GPP_ERR_SHAPE, "windowed attention: rows must equal micro_batch*seq_len");
         if (d.head_dim > window_max_head_dim()) FAIL(GPP_ERR_UNSUPPORTED, "windowed attention: head dimension above 256");
         if (d.seq_len > (1 << 30)) FAIL(GPP_ERR_UNSUPPORTED, "windowed attention: sequence too long for this build");
-        if (nd.rows * (int64_t)d.heads > (1 << 25)) FAIL(GPP_ERR_UNSUPPORTED, "windowed attention: too many rows and heads");
+        // (a launch has fewer than 2^32 threads: 256 per four rows of a head at the most, 512 per block of keys)
+        if (nd.rows * (int64_t)d.heads > (1 << 25) || micro_batch * d.heads * ((d.seq_len + 3) / 4) > (1 << 23) ||
+            micro_batch * d.kv_heads * ((d.seq_len + 127) / 128) >= (1 << 23))
+          FAIL(GPP_ERR_UNSUPPORTED, "windowed attention: too many rows and heads");
         if (d.window < 0 || d.sinks < 0) FAIL(GPP_ERR_INVALID_ARG, "windowed attention: window and sinks must not be negative");
         if (d.causal != 0 && d.causal != 1) FAIL(GPP_ERR_INVALID_ARG, "windowed attention: causal is 0 or 1");
         // (as the kernels hold it: in fp32, times log2 e)

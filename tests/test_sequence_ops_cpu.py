@@ -175,6 +175,14 @@ def test_refusals_at_the_ends_of_ranges(lib):
     for scale in (1e-30, 1e30):
         d, keep = B.build_desc(_changed(ops, 1, scale=scale), 4)
         assert B.gpp_stage_workspace_bytes(d) > 0
+    b = 1 << 20
+    for heads, want in ((16, B.GPP_ERR_UNSUPPORTED), (8, B.GPP_ERR_UNSUPPORTED), (7, None)):      # single tokens: workgroups of a launch
+        ops = S.attention_ops(b, 1, heads, heads, 8)
+        if want is not None:
+            assert _status(ops, b) == want
+        else:
+            d, keep = B.build_desc(ops, b)
+            assert B.gpp_stage_workspace_bytes(d) > 0
     with pytest.raises(ValueError):
         B.build_desc(S.rotary_ops(4, 16, 6, 64, (1, 1, 1, 1, 1)), 4)
     assert _status(S.rotary_ops(1, 1 << 29, 1, 2, (1,)), 1) == B.GPP_ERR_UNSUPPORTED      # more workgroups than a launch has
