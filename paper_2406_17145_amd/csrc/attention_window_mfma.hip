@@ -286,7 +286,8 @@ __device__ __forceinline__ uint32_t win_bits(int first, int end, int sinks) {
   return ((win_low_bits(end) & ~win_low_bits(first)) | win_low_bits(sinks)) >> (4 * ((threadIdx.x & 63) >> 5));
 }
 __device__ __forceinline__ float win_keep_bit(float v, uint32_t bits, int r, float hidden) {
-  const uint32_t t = (uint32_t)((int32_t)(bits << (31 - (8 * (r >> 2) + (r & 3)))) >> 31);
+  uint32_t t = (uint32_t)((int32_t)(bits << (31 - (8 * (r >> 2) + (r & 3)))) >> 31);
+  asm("" : "+v"(t));      // (taken for a condition, it becomes a comparison and a choice: four instructions)
   return __uint_as_float((__float_as_uint(v) & t) | (__float_as_uint(hidden) & ~t));
 }
 
@@ -645,9 +646,11 @@ __device__ __forceinline__ void win_dq_body(const WindowProb &p, const ExtPtrs &
   if (keys.count == 1) keys.end = keys.first = keys.sink_end = 0;      // a single key's probability is constant: no gradient
   const float scale2 = p.scale * LOG2E;
   const float lse = q0 < len ? p.lse[stat] : 0.0f;
-  f32x16 dq[C::DB];
+  f32x16 dq[C::DB], minus;      // (dP's products are added to -delta)
 #pragma unroll
   for (int d = 0; d < C::DB; ++d) dq[d] = win_zero();
+#pragma unroll
+  for (int r = 0; r < 16; ++r) minus[r] = -delta;
 
   win_stream_keys<Q>(tiles, nt, stream, lds, wave, co, lds0,
                          [&](const unsigned char *tk, const unsigned char *tv, int k0) {
@@ -656,14 +659,14 @@ __device__ __forceinline__ void win_dq_body(const WindowProb &p, const ExtPtrs &
       if (KG == 2 && u != kg) continue;
       const int sees = mine.sees(k0 + 32 * u, 32);
       if (sees == WIN_NONE) continue;
-      f32x16 st = win_zero(), dp = win_zero();
+      f32x16 st = win_zero(), dp = minus;
 #pragma unroll
       for (int s = 0; s < C::KS; ++s) {
         st = F::mma(win_row_frag<T, DH>(at, tk, 32 * u, s), qf.f[s], st);
         dp = F::mma(win_row_frag<T, DH>(at, tv, 32 * u, s), gf.f[s], dp);
       }
 #pragma unroll
-      for (int r = 0; r < 16; ++r) st[r] = __builtin_amdgcn_exp2f(fmaf(st[r], scale2, -lse)) * (dp[r] - delta);
+      for (int r = 0; r < 16; ++r) st[r] = __builtin_amdgcn_exp2f(fmaf(st[r], scale2, -lse)) * dp[r];
       if (sees == WIN_SOME) {
         asm volatile("");
         const int j = k0 + 32 * u;
