@@ -47,10 +47,11 @@ __device__ __forceinline__ int win_swizzle(int row) {
   return RB == 128 ? (((row >> 1) & 1) << 2) | (((row >> 2) & 1) << 1) : (RB == 256 ? (row & 3) << 2 : (row & 1) << 3);
 }
 
-template <typename T, int DH>
+// (KG: waves that share 32 rows and take 32 rows of a tile each)
+template <typename T, int DH, int KG = 1>
 struct WinTile {
   static constexpr int ES = sizeof(T), RB = DH * ES <= 128 ? 128 : (DH * ES <= 256 ? 256 : 512), CPR = RB / 16, EPC = 16 / ES;
-  static constexpr int KT = RB == 512 ? 32 : 64;     // rows of a streamed tile (fp32 rows of 512 bytes: two buffers of two tiles are 65 KB)
+  static constexpr int KT = RB == 512 && KG == 1 ? 32 : 64;     // rows of a streamed tile (fp32 rows of 512 bytes: two buffers of two tiles are 65 KB)
   static constexpr int GROUP = 1040, RPG = 1024 / RB;
   static constexpr int SUB = KT / 32, BYTES = KT / RPG * GROUP;
   static constexpr int KS = DH / 16, DB = DH / 32;
@@ -216,16 +217,16 @@ __device__ __forceinline__ float win_half_sum(float v) {
 
 // ---- copies into LDS -----------------------------------------------------------------------------------------
 // where this lane's pieces of a tile lie behind the tile's first row: copy q of wave w of NW fills the KB w * N + q of the tile
-template <typename T, int DH, int NW>
+template <typename T, int DH, int NW, int KG = 1>
 struct WinCopy {
-  static constexpr int N = WinTile<T, DH>::KT / WinTile<T, DH>::RPG / NW;
+  static constexpr int N = WinTile<T, DH, KG>::KT / WinTile<T, DH>::RPG / NW;
   uint32_t off[N];
 };
-template <typename T, int DH, int NW>
-__device__ __forceinline__ WinCopy<T, DH, NW> win_copy_offsets(int wave, int64_t ld, int dh) {
+template <typename T, int DH, int NW, int KG = 1>
+__device__ __forceinline__ WinCopy<T, DH, NW, KG> win_copy_offsets(int wave, int64_t ld, int dh) {
   typedef WinTile<T, DH> C;
   const int l = threadIdx.x & 63;
-  WinCopy<T, DH, NW> r;
+  WinCopy<T, DH, NW, KG> r;
 #pragma unroll
   for (int q = 0; q < r.N; ++q) {
     const int row = (wave * r.N + q) * C::RPG + l / C::CPR, c = (l % C::CPR) ^ win_swizzle<C::RB>(row);
@@ -239,8 +240,8 @@ __device__ __forceinline__ rsrc4 win_rsrc(const GPP_G void *base, uint32_t bytes
                  (uint32_t)__builtin_amdgcn_readfirstlane((int)((uint32_t)(a >> 32) & 0xffffu)),
                  (uint32_t)__builtin_amdgcn_readfirstlane((int)bytes), 0x00020000u};
 }
-template <typename T, int DH, int NW>
-__device__ __forceinline__ void win_copy(rsrc4 rs, const WinCopy<T, DH, NW> &o, uint32_t dst, int wave) {
+template <typename T, int DH, int NW, int KG>
+__device__ __forceinline__ void win_copy(rsrc4 rs, const WinCopy<T, DH, NW, KG> &o, uint32_t dst, int wave) {
 #pragma unroll
   for (int q = 0; q < o.N; ++q) lds_copy16(rs, dst + (wave * o.N + q) * WinTile<T, DH>::GROUP, o.off[q]);
 }
@@ -307,9 +308,9 @@ __device__ __forceinline__ WinRange win_range(const WindowProb &p, int q0, int q
   return r;
 }
 // The tiles of K and V of a block of queries one after the other, each pair to LDS byte `dst`
-template <typename T, int DH>
+template <typename T, int DH, int KG>
 struct WinKeyStream {
-  typedef WinTile<T, DH> C;
+  typedef WinTile<T, DH, KG> C;
   const GPP_G T *k;             // the next tile of keys
   int64_t ld, step, v;          // row stride; elements from tile to tile, from K to V
   int sinks, rows;              // tiles until the jump to the window; rows of the sample from the next tile on
@@ -328,7 +329,7 @@ struct WinKeyStream {
     tail = win_tile_bytes((len - 1) % C::KT + 1, ld, dh, C::ES);
   }
   template <int NW>
-  __device__ __forceinline__ void copy(const WinCopy<T, DH, NW> &co, uint32_t dst, int wave) {
+  __device__ __forceinline__ void copy(const WinCopy<T, DH, NW, KG> &co, uint32_t dst, int wave) {
     const uint32_t bytes = rows >= C::KT ? whole : tail;
     rsrc4 rk = win_rsrc(k, bytes), rv = win_rsrc(k + v, bytes);
     settle(rk, rv);
@@ -447,7 +448,7 @@ struct WinKeep {
 // each; for launches of so few blocks that they would leave compute units idle.
 template <typename T, int DH, int NW, int KG>
 struct WinQueryCfg {
-  typedef WinTile<T, DH> C;
+  typedef WinTile<T, DH, KG> C;
   static constexpr int QG = NW / KG, ROWS = 32 * QG;
   static constexpr int NB = C::RB == 128 ? 3 : 2;                                  // buffers: as many as leave room for two workgroups' waves
   static constexpr int CP = 2 * C::KT / C::RPG / NW;                               // copies of a wave per step
@@ -456,10 +457,10 @@ struct WinQueryCfg {
 };
 
 // What forward and dQ do with their tiles of K and V: a ring of NB buffers; step(K tile, V tile, first key)
-template <typename Q, typename T, int DH, int NW, typename Step>
-__device__ __forceinline__ void win_stream_keys(const WinRange &tiles, int nt, WinKeyStream<T, DH> &stream, const unsigned char *lds, int wave,
-                                                const WinCopy<T, DH, NW> &co, uint32_t lds0, const Step &step) {
-  typedef WinTile<T, DH> C;
+template <typename Q, typename Stream, typename Copy, typename Step>
+__device__ __forceinline__ void win_stream_keys(const WinRange &tiles, int nt, Stream &stream, const unsigned char *lds, int wave, const Copy &co,
+                                                uint32_t lds0, const Step &step) {
+  typedef typename Q::C C;
   uint32_t in = 2 * (Q::NB - 1) * C::BYTES, out = 0;       // buffers of the next copy and of this step
   for (int t = 0; t < nt; ++t) {
     if (Q::NB > 2 && t + Q::NB - 1 <= nt) copies_landed_barrier<(Q::NB - 2) * Q::CP>();
@@ -478,7 +479,7 @@ __device__ __forceinline__ void win_stream_keys(const WinRange &tiles, int nt, W
 // the partner lane holds.
 template <typename T, int DH, int KG>
 __global__ __launch_bounds__(256, 2) void k_window_fwd_mfma(const WindowProb *__restrict__ probs, int n, ExtPtrs ext, StageFlags *flags) {
-  typedef WinTile<T, DH> C;
+  typedef WinTile<T, DH, KG> C;
   typedef WinFrag<T> F;
   typedef WinQueryCfg<T, DH, 4, KG> Q;
   constexpr int ROWS = Q::ROWS;
@@ -494,9 +495,9 @@ __global__ __launch_bounds__(256, 2) void k_window_fwd_mfma(const WindowProb *__
   const GPP_G T *kbase = qkv + row0 * p.ld_qkv + (int64_t)(p.heads + w.g) * p.dh;
   const int q0 = w.r0 + 32 * qg, q = q0 + (lane & 31), qc = max(0, min(q, len - 1));
   const WinRange tiles = win_range<C::KT>(p, w.r0, min(w.r0 + ROWS, len) - 1, len);
-  const WinCopy<T, DH, 4> co = win_copy_offsets<T, DH, 4>(wave, p.ld_qkv, p.dh);
+  const WinCopy<T, DH, 4, KG> co = win_copy_offsets<T, DH, 4, KG>(wave, p.ld_qkv, p.dh);
   const uint32_t lds0 = lds_address((const uint16_t *)lds);
-  WinKeyStream<T, DH> stream(kbase, (int64_t)p.kv_heads * p.dh, p.ld_qkv, p.dh, tiles, len);
+  WinKeyStream<T, DH, KG> stream(kbase, (int64_t)p.kv_heads * p.dh, p.ld_qkv, p.dh, tiles, len);
 #pragma unroll
   for (int k = 0; k < Q::NB - 1; ++k)
     if (k < tiles.n) stream.copy(co, lds0 + 2 * k * C::BYTES, wave);
@@ -609,7 +610,7 @@ __global__ __launch_bounds__(256, 2) void k_window_fwd_mfma(const WindowProb *__
 // (`local`: block of queries of the record; `lds`: Q::LDS bytes.  DELTA: the deltas are written for the dK / dV kernel behind this one)
 template <typename T, int DH, int NW, int KG, bool DELTA>
 __device__ __forceinline__ void win_dq_body(const WindowProb &p, const ExtPtrs &ext, int local, unsigned char *lds) {
-  typedef WinTile<T, DH> C;
+  typedef WinTile<T, DH, KG> C;
   typedef WinFrag<T> F;
   typedef WinQueryCfg<T, DH, NW, KG> Q;
   constexpr int ROWS = Q::ROWS;
@@ -623,9 +624,9 @@ __device__ __forceinline__ void win_dq_body(const WindowProb &p, const ExtPtrs &
   const WinRange tiles = win_range<C::KT>(p, w.r0, min(w.r0 + ROWS, len) - 1, len);
   GPP_G void *dqkv = p.ext_out >= 0 ? (GPP_G void *)ext.p[p.ext_out] : p.out;
   const int nt = dqkv ? tiles.n : 0;
-  const WinCopy<T, DH, NW> co = win_copy_offsets<T, DH, NW>(wave, p.ld_qkv, p.dh);
+  const WinCopy<T, DH, NW, KG> co = win_copy_offsets<T, DH, NW, KG>(wave, p.ld_qkv, p.dh);
   const uint32_t lds0 = lds_address((const uint16_t *)lds);
-  WinKeyStream<T, DH> stream(kbase, (int64_t)p.kv_heads * p.dh, p.ld_qkv, p.dh, tiles, len);
+  WinKeyStream<T, DH, KG> stream(kbase, (int64_t)p.kv_heads * p.dh, p.ld_qkv, p.dh, tiles, len);
 #pragma unroll
   for (int k = 0; k < Q::NB - 1; ++k)
     if (k < nt) stream.copy(co, lds0 + 2 * k * C::BYTES, wave);
@@ -1017,14 +1018,14 @@ template <typename T, int DH>
 __global__ __launch_bounds__((WinKeyCfg<T, DH, true>::NW * 64), (DH * sizeof(T) <= 256 ? 2 : 1)) void k_window_bwd_mfma(const WindowProb *__restrict__ probs,
                                                                                                              int n, ExtPtrs ext) {
   typedef WinKeyCfg<T, DH, true> K;
-  typedef WinQueryCfg<T, DH, K::NW, WinTile<T, DH>::SUB> Q;
+  typedef WinQueryCfg<T, DH, K::NW, 2> Q;
   __shared__ __attribute__((aligned(16))) unsigned char lds[K::LDS > Q::LDS ? K::LDS : Q::LDS];
   const int pi = find_prob(probs, n, blockIdx.x);
   const WindowProb p = probs[pi];
   win_fetch(p);
   const int local = blockIdx.x - p.blk_begin;
   if (local < p.units) win_dkv_body<T, DH, true>(p, ext, local, lds);
-  else win_dq_body<T, DH, K::NW, WinTile<T, DH>::SUB, false>(p, ext, local - p.units, lds);
+  else win_dq_body<T, DH, K::NW, 2, false>(p, ext, local - p.units, lds);
 }
 
 // The sums of a split block's parts, in order: four columns of a key per thread, DH / 4 workgroups per block (bound by memory; 12 us for
@@ -1101,11 +1102,14 @@ static int window_tile_rows(const WindowProb &p, int dh) { return dh * (p.dtype 
 // Two waves per 32 queries where the blocks of 128 do not give every compute unit one, in fp32 two, whose products take sixteen times as
 // long.  Step of 2 samples, bf16, heads of 64, window 128 / all earlier keys: 256 blocks 52 -> 48 / 88 -> 77 us, 512 blocks 70 -> 74 /
 // 171 -> 161; heads of 128, window 256: 256 blocks 85 -> 82, 512 blocks 99 -> 112; fp32: 128 blocks 75 -> 63, 512 blocks 182 -> 175.
+// In fp32 with heads of more than 64 columns two waves take a compute unit's whole LDS for their tiles of 64 keys: 1 x 2000 causal, heads of
+// 128, 128 blocks 874 -> 612, heads of 96, 192 blocks 467 -> 378, 256 blocks 202 -> 220.
 int window_key_groups(const WindowProb &p, int dh, int64_t blocks) {
-  return window_tile_rows(p, dh) == 64 && blocks <= (p.dtype == DT_BF16 ? 256 : 512) ? 2 : 1;
+  return blocks <= (p.dtype == DT_BF16 ? 256 : window_tile_rows(p, dh) == 64 ? 512 : 192) ? 2 : 1;
 }
 // whether the backward pass is one launch: its workgroups, one per compute unit, all run at once
 bool window_one_backward(int64_t workgroups) { return workgroups <= 256; }
+int window_one_rows(const WindowProb &p, int dh) { return window_tile_rows(p, dh) == 64 ? 128 : 64; }      // queries of a workgroup: 8 waves or 4, two for 32
 // The same where blocks of keys, none of them split, leave half of the compute units to the blocks of queries (fewer steps than parts
 // are made of: short samples, heads that share keys).  Step of 8 samples of 128 in bf16, 32 heads over 8: heads of 64 33.9 -> 27.9 us,
 // of 128 51.1 -> 42.1, over 16 30.2 -> 26.2; as many units as compute units (over 32) 45.7 -> 48.4 with heads of 128; 512 blocks of
@@ -1211,8 +1215,7 @@ int window_key_slots(int dtype, int dh) { return dtype == DT_BF16 && dh == 32 ? 
       else GO(float, 128);                \
     }                                     \
   } while (0)
-// (tiles of 32 keys are not shared: WinTile::SUB key groups at the most)
-#define WIN_QUERY_KERNEL(K, T, DH) (key_groups == 2 ? K<T, DH, WinTile<T, DH>::SUB> : K<T, DH, 1>)
+#define WIN_QUERY_KERNEL(K, T, DH) (key_groups == 2 ? K<T, DH, 2> : K<T, DH, 1>)
 
 void launch_window_fwd_mfma(const WindowProb *probs, int n, int total_blocks, int dtype, int dh, int key_groups, const ExtPtrs &ext, StageFlags *flags,
                             hipStream_t s) {

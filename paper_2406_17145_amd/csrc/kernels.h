@@ -379,6 +379,7 @@ int window_mfma_dh(const WindowProb &p);
 // key groups of a launch of `blocks` blocks of 128 queries: how many waves share 32 queries
 int window_key_groups(const WindowProb &p, int dh, int64_t blocks);
 bool window_one_backward(int64_t workgroups);
+int window_one_rows(const WindowProb &p, int dh);
 bool window_keys_first(int dtype, int dh, int64_t query_blocks);
 bool window_beside(int64_t query_blocks, int64_t key_units);
 void window_plan_queries(WindowProb &p, int rows);      // blocks of `rows` queries

@@ -797,11 +797,14 @@ struct Emitter {
         if (now.empty()) continue;
         int64_t blocks128 = 0;
         for (auto &a : now) blocks128 += (int64_t)a.batch * a.heads * ((a.seq + 127) / 128);
+        const int one_rows = dh ? window_one_rows(now[0], dh) : 128;
+        int64_t one_blocks = 0;
+        for (auto &a : now) one_blocks += (int64_t)a.batch * a.heads * ((a.seq + one_rows - 1) / one_rows);
         const int groups = dh ? window_key_groups(now[0], dh, blocks128) : 1;
-        // (the branches of a level share the GPU; in one launch the blocks of keys take what the blocks of 128 queries leave)
-        bool one = dh && backward && window_one_backward(2 * blocks128);
+        // (the branches of a level share the GPU; in one launch the blocks of keys take what the blocks of queries leave)
+        bool one = dh && backward && window_one_backward(2 * one_blocks);
         auto plan_keys = [&] {
-          const int slots = std::max(1, (int)((one ? 256 - blocks128 : window_key_slots(dt, dh)) / (int64_t)now.size()));
+          const int slots = std::max(1, (int)((one ? 256 - one_blocks : window_key_slots(dt, dh)) / (int64_t)now.size()));
           bool fits = true;
           for (auto &a : now) {
             window_plan_queries(a, 128);
@@ -821,9 +824,9 @@ struct Emitter {
             units += a.units;
             joins += window_join_blocks(a, dh);
           }
-          one = joins == 0 && window_beside(blocks128, units);
+          one = joins == 0 && window_beside(one_blocks, units);
         }
-        for (auto &a : now) window_plan_queries(a, one ? 128 : 128 / groups);
+        for (auto &a : now) window_plan_queries(a, one ? one_rows : 128 / groups);
         auto queries = [&](const WindowProb &a) { return dh ? a.query_units : window_blocks(a.batch, a.heads, a.seq); };
         if (!backward) {
           step(K_WINDOW_FWD, now, dt, dh, groups, queries);

@@ -75,6 +75,15 @@ def test_window_ragged(window, sinks, causal, dtype, fill):
                   values=[0, 140, 1, 77, 128], fill=fill)
 
 
+@pytest.mark.parametrize("dh", [80, 128])
+@pytest.mark.parametrize("b,seq,window,sinks,causal", [(1, 700, 0, 0, True), (2, 420, 90, 3, False), (3, 70, 33, 2, True), (13, 520, 40, 0, True)])
+def test_window_wide_rows_of_fp32(dh, b, seq, window, sinks, causal):
+    """Heads of more than 64 columns in fp32: few blocks of queries, whose waves share them, and (13 samples) many."""
+    run_attention(b=b, seq=seq, heads=4, kv=2, dh=dh, window=window, sinks=sinks, causal=causal, dtype="f32")
+    run_attention(b=b, seq=seq, heads=4, kv=2, dh=dh, window=window, sinks=sinks, causal=causal, dtype="f32",
+                  values=[seq, 1, 0, seq // 2, 65][:b] + [seq - 33] * max(0, b - 5))
+
+
 def test_window_all_samples_empty():
     ops = S.attention_ops(2, 40, 2, 1, 64, lengths=True)
     batch, gout = S.draw(ops, 2, 1, lengths([0, 0]))
