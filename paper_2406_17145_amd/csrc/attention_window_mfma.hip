@@ -19,11 +19,11 @@
 // queries that are split over workgroups meet in a fixed order.
 //
 // What bounds it.  Long rows: matrix cores and vector unit (exponentials, masks, conversions) of a SIMD's two waves are busy half of the
-// time each, and the clock falls under the load.  1 x 16384, window 4096, causal, 16 heads of 128 over 2, bf16: forward 573 us
-// (0.84 PFLOP/s of visible pairs, matrix cores busy 52 %), dQ 758 (0.95, 58 %), dK and dV 1016 - 1091 (0.9, 55 %), joining 12.  Heads of
-// 64: twice the vector work per product; 2 x 8192, window 1024, causal, 16 heads over 4: a step of 416 us, 0.70 PFLOP/s where
-// heads of 128 reach 0.95.  Short rows: a wave's chain through a tile, some 2000 cycles, between a launch's first loads and last stores; 4 x 512, window 128, 16 heads of
-// 64 over 4: forward 14 us, dK and dV 21, dQ and the joining 14.
+// time each, and the clock falls under the load.  1 x 16384, window 4096, causal, 16 heads of 128 over 2, bf16: forward 572 us
+// (0.84 PFLOP/s of visible pairs, matrix cores busy 52 %), dQ 731 - 744 (0.98, 59 %), dK and dV 1036 - 1104 (0.9, 55 %), joining 12.  Heads of
+// 64: twice the vector work per product; 2 x 8192, window 1024, causal, 16 heads over 4: a step of 407 us, 0.71 PFLOP/s where
+// heads of 128 reach 0.98.  Short rows: a wave's chain through a tile, some 2000 cycles, between a launch's first loads and last stores;
+// 4 x 512, window 128, 16 heads of 64 over 4: forward 13 - 14 us, dK and dV 20, dQ and the joining 13.
 #include <algorithm>
 
 #include "gemm_direct.h"
