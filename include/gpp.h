@@ -94,7 +94,8 @@ typedef enum {
                                last head_dim - 2 P columns of a block are not rotated.  Pair i, the j-th of axis a, turns by
                                position[a] * w radians: (x0, x1) -> (x0 cos - x1 sin, x0 sin + x1 cos), w = base^(-i/P) on one
                                ladder of frequencies, base^(-j/axis_pairs[a]) on a ladder per axis.  Angles are formed and
-                               reduced in 64 bits.  out_features = features of x; the output has x's dtype */
+                               reduced in 64 bits.  out_features = features of x; the output has x's dtype.  P up to 512, rows
+                               up to 2^25 (up to 2^27 where P is at most 128) */
   GPP_OP_ATTENTION_WINDOW = 14 /* attention inside a window, with first tokens that stay visible.  in[0] = [b*S, (heads +
                                2*kv_heads)*head_dim] as Q|K|V column blocks; query head h reads key / value head
                                h / (heads / kv_heads).  Query i of a sample sees key j when (not causal or j <= i) and
@@ -102,7 +103,7 @@ typedef enum {
                                S each); rows of a sample at and behind its length are padding: not read, output and
                                gradients zero.  out_features = heads*head_dim, S = seq_len.  The values of rows that are not
                                padding have to be finite: a key's NaN or infinity may reach queries that do not see it.
-                               head_dim up to 256, rows * heads up to 2^25, samples * heads up to 2^23.
+                               head_dim up to 256, b * heads * ceil(S / 4) up to 2^23, b * kv_heads * ceil(S / 128) below 2^23.
                                A caller's tensor that either operator writes must not overlap one that it reads */
 } gpp_op_kind_t;
 

@@ -1151,6 +1151,8 @@ void window_plan_parts(WindowProb &p, int dh, int slots, bool one_round) {
     const int64_t rest = blocks - whole, parts = up(regular, part), sink_parts = sb ? up(every, part) : 1;
     const int64_t split = (parts > 1 ? rest * parts : 0) + (sink_parts > 1 ? bg * sb * sink_parts : 0);
     const int64_t units = whole + rest * parts + bg * sb * sink_parts;
+    // (fewer than 2^32 threads in this launch and in the joining one; blocks that are not split always fit)
+    if (units >= (1 << 23) || dh / 4 * ((parts > 1 ? rest : 0) + (sink_parts > 1 ? bg * sb : 0)) >= (1 << 23)) return;
     const double slot = (steps + start * (double)units) / slots;
     const double longest = std::max(whole ? (double)regular : 0.0, (double)std::min(part, std::max(rest ? regular : 0, sb ? every : 0))) + start;
     double t = std::max(slot, longest);

@@ -169,7 +169,8 @@ gpp_status_t Plan::analyse(const gpp_stage_desc_t *desc) {
         if (d.seq_len <= 0 || nd.rows != micro_batch * d.seq_len) FAIL(GPP_ERR_SHAPE, "windowed attention: rows must equal micro_batch*seq_len");
         if (d.head_dim > window_max_head_dim()) FAIL(GPP_ERR_UNSUPPORTED, "windowed attention: head dimension above 256");
         if (d.seq_len > (1 << 30)) FAIL(GPP_ERR_UNSUPPORTED, "windowed attention: sequence too long for this build");
-        // (a launch has fewer than 2^32 threads: 256 per four rows of a head at the most, 512 per block of keys)
+        // (a launch has fewer than 2^32 threads: 256 per four rows of a head at the most, 512 per block of keys; of several operators see
+        // add_launches())
         if (nd.rows * (int64_t)d.heads > (1 << 25) || micro_batch * d.heads * ((d.seq_len + 3) / 4) > (1 << 23) ||
             micro_batch * d.kv_heads * ((d.seq_len + 127) / 128) >= (1 << 23))
           FAIL(GPP_ERR_UNSUPPORTED, "windowed attention: too many rows and heads");
@@ -729,6 +730,26 @@ struct Emitter {
     r.ext_x = r.ext_y = r.ext_pos = -1;
     return r;
   }
+  // Records of one kernel in launches of fewer than 2^23 workgroups (of up to 512 threads; a launch has fewer than 2^32): one launch but
+  // for very many rows.  A record alone never has too many, analyse() refuses it.  `set` fills in a step of its launch.
+  template <typename T, typename Blocks, typename Set>
+  void add_launches(int kern, std::vector<T> &recs, const Blocks &blocks_of, const Set &set) {
+    std::vector<T> now;
+    int64_t blocks = 0;
+    auto launch = [&] {
+      if (blocks > 0) set(add_step(kern, push_table(now), (int)now.size(), (int)blocks));
+      now.clear();
+      blocks = 0;
+    };
+    for (auto &r : recs) {
+      const int64_t more = blocks_of(r);
+      if (blocks > 0 && blocks + more >= (1 << 23)) launch();
+      r.blk_begin = (int32_t)blocks;
+      blocks += more;
+      now.push_back(r);
+    }
+    launch();
+  }
   // one launch per storage type and width of a lane's piece
   void emit_rotaries(std::vector<RotaryProb> &recs) {
     int64_t rows = 0;
@@ -736,19 +757,17 @@ struct Emitter {
     for (int32_t dt : {DT_F32, DT_BF16})
       for (int vec = 8; vec >= 1; vec >>= 1) {
         std::vector<RotaryProb> now;
-        int blocks = 0;
         for (auto &r : recs) {
           if (r.dtype != dt || rotary_vec(r) != vec) continue;
           r.rows_per_block = rotary_rows_per_block(rows, r.pairs);
-          r.blk_begin = blocks;
-          blocks += (r.rows + r.rows_per_block - 1) / r.rows_per_block;
           now.push_back(r);
         }
-        if (now.empty()) continue;
-        Step &s = add_step(K_ROTARY, push_table(now), (int)now.size(), blocks);
-        s.ext_kind = EXT_BOTH;
-        s.a0 = dt;
-        s.a1 = vec;
+        add_launches(K_ROTARY, now, [](const RotaryProb &r) { return ((int64_t)r.rows + r.rows_per_block - 1) / r.rows_per_block; },
+                     [&](Step &s) {
+                       s.ext_kind = EXT_BOTH;
+                       s.a0 = dt;
+                       s.a1 = vec;
+                     });
       }
     recs.clear();
   }
@@ -777,17 +796,12 @@ struct Emitter {
   void emit_windows(std::vector<WindowProb> &recs, bool backward) {
     auto mfma_dh = [&](const WindowProb &a) { return (pl.flags & 1) || (backward && a.grad_dtype != a.dtype) ? 0 : window_mfma_dh(a); };
     auto step = [&](int kern, std::vector<WindowProb> &now, int dtype, int dh, int groups, auto blocks_of) {
-      int blocks = 0;
-      for (auto &a : now) {
-        a.blk_begin = blocks;
-        blocks += blocks_of(a);
-      }
-      if (blocks == 0) return;
-      Step &s = add_step(kern, push_table(now), (int)now.size(), blocks);
-      s.ext_kind = EXT_BOTH;
-      s.a0 = dtype;
-      s.a1 = dh;
-      s.a2 = groups;
+      add_launches(kern, now, blocks_of, [&](Step &s) {
+        s.ext_kind = EXT_BOTH;
+        s.a0 = dtype;
+        s.a1 = dh;
+        s.a2 = groups;
+      });
     };
     for (int32_t dt : {DT_F32, DT_BF16})
       for (int dh : {0, 32, 64, 96, 128}) {

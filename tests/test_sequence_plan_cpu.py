@@ -1,0 +1,51 @@
+"""Plans of stages with several sequence operators (rotary positions, windowed attention), without a GPU: launches and memory."""
+import pytest
+
+from paper_2406_17145_amd import binding as B
+from tests import sequence_util as S
+
+
+@pytest.fixture(scope="module")
+def lib():
+    import os
+    if not os.path.exists(B.LIB_PATH):
+        from paper_2406_17145_amd.build import build_library
+        build_library(verbose=False)
+    return B.load()
+
+
+def branches(one, n):
+    """n copies of an operator graph beside each other."""
+    return [{**op, "inputs": [p + k * len(one) for p in op["inputs"]]} for k in range(n) for op in one]
+
+
+def launches(ops, b):
+    d, keep = B.build_desc(ops, b)
+    return [s for s in B.gpp_stage_describe(d) if s["kernel"] != "loss_sum"]
+
+
+@pytest.mark.parametrize("op", ["attention", "attention of one type on the matrix cores", "rotary"])
+@pytest.mark.parametrize("grad", [False, True])
+def test_launches_of_many_records_stay_below_2_to_the_32_threads(lib, op, grad):
+    """Each of the three branches may have a launch of its own (7 * 2^20 workgroups of up to 512 threads, rotary 2^23 - 2^16 of 256);
+    one launch of all three would have 5.6e9 threads or more."""
+    b = 1 << 20
+    if op == "rotary":
+        one, threads, each = S.rotary_ops(b, 127, 1, 2, (1,), grad=grad), 256, 127 * b // 16
+    else:
+        mixed = op == "attention"
+        one = S.attention_ops(b, 1, 7, 7, 12 if mixed else 8, grad=grad)
+        threads, each = (256 if mixed else 512), 7 * b
+    for n in (1, 2, 3):
+        steps = launches(branches(one, n), b)
+        for direction in ("forward", "backward") if grad else ("forward",):
+            here = [s for s in steps if s["pass"] == direction]
+            assert here and all(s["blocks"] * threads < 1 << 32 for s in here)
+            for kernel in {s["kernel"] for s in here}:
+                mine = [s for s in here if s["kernel"] == kernel]
+                assert sum(s["records"] for s in mine) == n and sum(s["blocks"] for s in mine) == n * each
+
+
+def test_branches_share_a_launch_where_they_fit(lib):
+    for one in (S.attention_ops(4, 100, 4, 2, 64, window=9), S.rotary_ops(4, 100, 6, 64, (8, 12, 12))):
+        assert [s["records"] for s in launches(branches(one, 5), 4)] == [5, 5]
