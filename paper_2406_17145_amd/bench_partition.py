@@ -47,6 +47,8 @@ def op_costs(wl):
             first = min(op.get("sinks", 0), s - near)
             pairs = (s * near - near * (near - 1) / 2) * (1 if causal else 2) - (0 if causal else s)    # of a query and a key in its window
             pairs += first * (s - near) - first * (first - 1) / 2                                      # and a first token in front of it
+            ahead = 0 if causal else max(0, min(op.get("sinks", 0), s) - near)
+            pairs += ahead * (ahead + 1) / 2                                                           # or behind it
             flops = 4.0 * 3.5 * pairs * feat
             bytes_ = 4 * r * feat * (1 + 2 * op["kv_heads"] / op["heads"]) * e + 4 * r * feat * e
         elif k == "embedding_bag_sum":

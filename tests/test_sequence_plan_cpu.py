@@ -49,3 +49,17 @@ def test_launches_of_many_records_stay_below_2_to_the_32_threads(lib, op, grad):
 def test_branches_share_a_launch_where_they_fit(lib):
     for one in (S.attention_ops(4, 100, 4, 2, 64, window=9), S.rotary_ops(4, 100, 6, 64, (8, 12, 12))):
         assert [s["records"] for s in launches(branches(one, 5), 4)] == [5, 5]
+
+
+@pytest.mark.parametrize("seq,window,sinks,causal", [(2048, 5, 300, False), (300, 20, 1000, False), (64, 64, 64, False), (64, 1, 64, False),
+                                                     (90, 7, 8, False), (2048, 5, 300, True), (300, 20, 1000, True)])
+def test_partition_costs_count_first_tokens_on_both_sides(monkeypatch, seq, window, sinks, causal):
+    """Queries see first tokens ahead of a two-sided window too (by the operations alone)."""
+    from types import SimpleNamespace
+    from oracle import gpp_oracle as O
+    from paper_2406_17145_amd import bench_partition as P
+    ops = S.attention_ops(1, seq, 8, 2, 128, window=window, sinks=sinks, causal=causal)
+    monkeypatch.setattr(P, "MEM_RATE", 1e30)
+    _, t, _, _ = P.op_costs(SimpleNamespace(ops=ops, micro_batch=1))
+    want = 4 * 3.5 * O.window_mask(seq, ops[1]).sum() * 1024 / P.MFMA_RATE
+    assert abs(t[1] - want) <= 1e-12 * want
