@@ -93,7 +93,7 @@ struct Plan {
   Buf fwd_scratch;
   int64_t fwd_scratch_bytes = 0;
   int64_t slot_bytes = 0, shared_bytes = 0, table_bytes = 0, tmp_bytes = 0;
-  int64_t gemm_partial_bytes = 0, gemm_counter_bytes = 0;   // split-K partial tiles and arrival counters
+  int64_t gemm_partial_bytes = 0, gemm_counter_bytes = 0;   // partial sums (split-K tiles; windowed attention's cut dK and dV) and arrival counters
   int64_t off_flags = 0, off_tables = 0, off_group_tables = 0, off_slots = 0, off_shared = 0, total_bytes = 0;
   // group launches (flag bits 8-11 = L): a second copy of the launch tables in which the records of the slots
   // l, l + L, l + 2L, ... follow each other, one table per lane l, so that ONE launch covers a step of several

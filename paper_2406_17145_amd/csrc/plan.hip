@@ -543,7 +543,7 @@ struct Emitter {
   std::vector<int> gstate;
   std::vector<Buf> gaddend;
   std::vector<char> dz_ready;
-  int64_t part_need = 0, cnt_need = 0;  // split-K scratch high-water marks over all launches
+  int64_t part_need = 0, cnt_need = 0;  // scratch of partial sums and counters of split contractions: high-water marks over all launches
   std::vector<LnProb> ln_fold_later;    // LayerNorm parameter folds of the whole backward pass (see backward())
   std::vector<GemmProb> dw_group;   // backward-weight records left to the launch over a group of slots
   std::vector<GemmProb> dw_later;   // backward-weight records left to one launch at the end of their own backward pass
@@ -846,16 +846,16 @@ struct Emitter {
           step(K_WINDOW_FWD, now, dt, dh, groups, queries);
           continue;
         }
-        if (dh)
-          for (auto &a : now) {
-            const int64_t bytes = window_partial_bytes(a, dh);
-            if (bytes == 0) continue;
-            Buf b;
-            b.space = SP_SHARED;
-            b.off = pl.shared_bytes + shared_tmp_top;
-            shared_tmp_top = align_up(shared_tmp_top + bytes, 256);
-            a.partial = (float *)ptr(b);
-          }
+        // (the sums are joined before any other launch that uses this scratch memory)
+        int64_t part_off = 0;
+        for (auto &a : now) {
+          const int64_t bytes = dh ? window_partial_bytes(a, dh) : 0;
+          if (bytes == 0) continue;
+          a.partial = (float *)(ws + pl.off_shared + pl.shared_bytes + pl.tmp_bytes + part_off);
+          part_off = align_up(part_off + bytes, 256);
+          pl.bwd_shared = true;
+        }
+        part_need = std::max(part_need, part_off);
         if (one) {
           step(K_WINDOW_BWD, now, dt, dh, 1, [&](const WindowProb &a) { return a.units + a.query_units; });
           step(K_WINDOW_JOIN, now, dt, dh, 1, [&](const WindowProb &a) { return window_join_blocks(a, dh); });

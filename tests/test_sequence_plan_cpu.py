@@ -63,3 +63,27 @@ def test_partition_costs_count_first_tokens_on_both_sides(monkeypatch, seq, wind
     _, t, _, _ = P.op_costs(SimpleNamespace(ops=ops, micro_batch=1))
     want = 4 * 3.5 * O.window_mask(seq, ops[1]).sum() * 1024 / P.MFMA_RATE
     assert abs(t[1] - want) <= 1e-12 * want
+
+
+def cut_sums(ops, b):
+    """Bytes of workspace beyond the tensors of a single attention whose gradient is wanted: its cut sums and, below 64 KB, tables."""
+    up = lambda v: (v + 63) // 64 * 64  # noqa: E731
+    x, a = ops[0], ops[-1]
+    rows, size = b * x["seq_len"], 2 if x["dtype"] == "bf16" else 4
+    d, keep = B.build_desc(ops, b)
+    return B.gpp_stage_workspace_bytes(d) - rows * (up(x["out_features"]) + up(a["out_features"])) * size - 2 * up(rows * a["heads"]) * 4
+
+
+def test_levels_share_the_memory_of_cut_sums(lib):
+    """Three attentions in a row: the parts of one are joined before those of the next are written."""
+    chain, parts, alone = [], [], []
+    for heads, kv in ((16, 4), (12, 2), (4, 4)):
+        one = S.attention_ops(4, 512, heads, kv, 64, window=100, causal=False)
+        d, keep = B.build_desc(one, 4)
+        alone.append(B.gpp_stage_workspace_bytes(d))
+        parts.append(cut_sums(one, 4))
+        chain = chain + [{**one[1], "inputs": [len(chain) - 1]}] if chain else one
+    assert sum(parts) - max(parts) > 8 << 20
+    d, keep = B.build_desc(chain, 4)
+    # (one's output is the next one's input: a gradient of it in the place of the copy of the caller's rows)
+    assert B.gpp_stage_workspace_bytes(d) <= sum(alone) - sum(parts) + max(parts) + (64 << 10)
