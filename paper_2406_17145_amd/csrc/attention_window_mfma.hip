@@ -783,7 +783,7 @@ __device__ __forceinline__ void win_dkv_body(const WindowProb &p, const ExtPtrs 
   GPP_G void *dqkv = p.ext_out >= 0 ? (GPP_G void *)ext.p[p.ext_out] : p.out;
   if (!dqkv) return;
   // (the unsplit units first, then the others)
-  const WinUnit w = win_unit(p, local < p.whole ? win_spread(local, p.whole, p.by_key_blocks) : p.whole + win_spread(local - p.whole, p.units - p.whole, p.by_key_blocks));
+  const WinUnit w = win_unit(p, local < p.whole ? win_spread(local, p.whole, p.by_key_blocks) : p.whole + win_spread(local - p.whole, p.units - p.whole, p.by_unit_run));
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), kg = wave & 3, qg = wave >> 2;
   const int len = __builtin_amdgcn_readfirstlane(window_length(p, w.b));
   const WinSteps st_ = win_steps<C::KT>(p, w.c0, len);
@@ -1133,6 +1133,13 @@ void window_plan_queries(WindowProb &p, int rows) {
 // their rounds; otherwise it is what a slot has to do, but no less than the rounds of whole blocks, plus half a part of unevenness.  A
 // unit costs the time of some steps for its operands and its result (4 us: about four steps of 64 x 128 pairs in bf16, half a
 // one in fp32), a part its sums' way through memory, the joining launch (5 us) the same for all.
+// The sums take 64 MB or twice the gradient's bytes, whichever is more; the estimate alone would have cut 1 x 32768 causal rows of fp32, 4
+// heads of 128 over 1, into 1074 MB of them.  In causal launches without a window, whose blocks hold less and less, many small parts only
+// evened out that a contiguous eighth of the units went to each XCD.  Runs of one block's parts go round the XCDs instead (win_spread),
+// and an odd number of them round the shader engines too (backward of that case: 2 / 4 / 8 parts 58 / 57 / 48 ms, 3 / 5 / 7 parts
+// 46.4 / 44.0 / 42.8; contiguous, 32 parts 44.5).  Backward with 5 to 9 parts in bounds and as many as the estimate took without: that
+// case 168 MB 44.0 ms, 1074 MB 44.5; bf16 8 heads of 128 over 1 168 MB 9.9 ms, 403 MB 10.7; 1 x 16384, 16 heads over 2 168 MB 4.54 ms,
+// 268 MB 5.67; fp32 8 heads over 1 151 MB 23.7 ms, 688 MB 22.4.
 // one_round: no more units than slots, if there is such a pair (units = 0: there is none).
 void window_plan_parts(WindowProb &p, int dh, int slots, bool one_round) {
   const int64_t kt = window_tile_rows(p, dh), group = p.heads / p.kv_heads, seq = p.seq, nb = (seq + WIN_ROWS - 1) / WIN_ROWS;
@@ -1145,6 +1152,8 @@ void window_plan_parts(WindowProb &p, int dh, int slots, bool one_round) {
   const bool wide = p.dtype != DT_BF16;
   const double start = wide ? 0.5 : 4.0, join = wide ? 0.75 : 6.0, sums = (wide ? 0.00005 : 0.00035) * dh;
   const double steps = (double)blocks * regular * (triangle ? 0.5 : 1.0) + (double)(bg * sb * every);
+  const int64_t bytes = (int64_t)p.batch * seq * (p.heads + 2 * p.kv_heads) * p.dh * (wide ? 4 : 2), unit_bytes = 2 * WIN_ROWS * dh * 4;
+  const int64_t most = std::max<int64_t>(64 << 20, 2 * bytes) / unit_bytes;
   double best = 1e300;
   p.units = 0;
   auto consider = [&](int64_t whole, int64_t part) {
@@ -1153,6 +1162,7 @@ void window_plan_parts(WindowProb &p, int dh, int slots, bool one_round) {
     const int64_t units = whole + rest * parts + bg * sb * sink_parts;
     // (fewer than 2^32 threads in this launch and in the joining one; blocks that are not split always fit)
     if (units >= (1 << 23) || dh / 4 * ((parts > 1 ? rest : 0) + (sink_parts > 1 ? bg * sb : 0)) >= (1 << 23)) return;
+    if (split && (units - whole > most || (triangle && parts % 2 == 0 && units > slots))) return;
     const double slot = (steps + start * (double)units) / slots;
     const double longest = std::max(whole ? (double)regular : 0.0, (double)std::min(part, std::max(rest ? regular : 0, sb ? every : 0))) + start;
     double t = std::max(slot, longest);
@@ -1188,6 +1198,7 @@ void window_plan_parts(WindowProb &p, int dh, int slots, bool one_round) {
   p.sink_blocks = (int32_t)sb;
   p.by_key_blocks = fast_div(nb - sb);
   p.by_parts = fast_div(p.parts);
+  p.by_unit_run = fast_div(triangle ? p.parts : nb - sb);
   p.by_sink_parts = fast_div(p.sink_parts);
   p.by_sink_blocks = fast_div(sb);
 }

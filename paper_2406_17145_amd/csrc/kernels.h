@@ -162,7 +162,7 @@ struct WindowProb {
   // first tokens (sink_blocks) into sink_parts
   GPP_G float *partial;    // fp32 sums of parts
   int32_t sink_blocks, sink_parts, parts, part_steps, whole, rest;
-  FastDiv by_group, by_kv_heads, by_query_blocks, by_run, by_key_blocks, by_parts, by_sink_parts, by_sink_blocks;   // matrix-core kernels
+  FastDiv by_group, by_kv_heads, by_query_blocks, by_run, by_key_blocks, by_parts, by_sink_parts, by_sink_blocks, by_unit_run;   // matrix-core kernels
   int32_t blk_begin;
 };
 

@@ -87,3 +87,14 @@ def test_levels_share_the_memory_of_cut_sums(lib):
     d, keep = B.build_desc(chain, 4)
     # (one's output is the next one's input: a gradient of it in the place of the copy of the caller's rows)
     assert B.gpp_stage_workspace_bytes(d) <= sum(alone) - sum(parts) + max(parts) + (64 << 10)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("causal,window,sinks", [(True, 0, 0), (False, 0, 0), (True, 700, 300), (False, 4000, 0)])
+@pytest.mark.parametrize("b,seq,heads,kv,dh", [(1, 32768, 4, 1, 128), (1, 32768, 2, 1, 32), (1, 23721, 8, 2, 32), (2, 4096, 8, 2, 128), (1, 16384, 16, 2, 128),
+                                               (3, 1500, 6, 3, 96), (5, 2000, 8, 1, 64), (1, 100000, 32, 1, 64), (64, 700, 4, 4, 80), (4, 512, 16, 4, 64)])
+def test_memory_of_cut_sums_is_bounded(lib, dtype, causal, window, sinks, b, seq, heads, kv, dh):
+    """64 MB or twice the gradient, whichever is more, and a megabyte for everything else."""
+    gradient = b * seq * (heads + 2 * kv) * dh * (2 if dtype == "bf16" else 4)
+    ops = S.attention_ops(b, seq, heads, kv, dh, window=window, sinks=sinks, causal=causal, dtype=dtype)
+    assert cut_sums(ops, b) <= max(64 << 20, 2 * gradient) + (1 << 20)
