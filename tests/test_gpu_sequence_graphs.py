@@ -39,6 +39,20 @@ def lengths(values):
     return {1: lambda r, s: np.resize(np.array(values), s)}
 
 
+@pytest.mark.parametrize("dtype,dh", [("bf16", 64), ("bf16", 128), ("bf16", 20), ("f32", 64), ("f32", 96)])
+@pytest.mark.parametrize("b,seq,heads,kv,window,sinks,causal,values", [
+    (2, 5, 4, 2, 3, 1, True, None), (3, 70, 4, 1, 0, 0, True, [70, 1, 33]), (2, 150, 6, 3, 17, 40, False, None), (2, 150, 2, 2, 64, 2, True, [150, 66]),
+    (1, 600, 4, 2, 100, 3, True, None), (4, 1, 2, 1, 0, 0, False, None)])
+def test_gradient_blocks(dtype, dh, b, seq, heads, kv, window, sinks, causal, values):
+    """dQ, dK and dV of each sample."""
+    ops = S.attention_ops(b, seq, heads, kv, dh, window=window, sinks=sinks, causal=causal, dtype=dtype, lengths=values is not None)
+    batch, gout = S.draw(ops, b, 21, lengths(values) if values else None)
+    got, ref = S.gpu(ops, b, batch, gout), S.oracle(ops, b, batch, gout)
+    for k in range(b):
+        rows = slice(k * seq, (k + 1) * seq)
+        check_blocks(f"sample {k}", got[1][rows], ref[1][rows], heads, kv, dh, dtype, seq)
+
+
 @pytest.mark.parametrize("b,seq,heads,kv,dh,dtype,values", [(3, 1500, 6, 3, 96, "f32", None), (5, 1300, 8, 1, 64, "bf16", None), (1, 3000, 8, 2, 128, "bf16", None),
                                                             (5, 1300, 8, 1, 64, "bf16", [1300, 0, 1, 700, 129])])
 def test_cut_blocks_of_causal_rows(b, seq, heads, kv, dh, dtype, values):
