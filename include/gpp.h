@@ -100,9 +100,12 @@ typedef enum {
                                2*kv_heads)*head_dim] as Q|K|V column blocks; query head h reads key / value head
                                h / (heads / kv_heads).  Query i of a sample sees key j when (not causal or j <= i) and
                                (window == 0 or |i - j| < window or j < sinks).  in[1], optional: lengths input (i32, [b, 1], 0 to
-                               S each); rows of a sample at and behind its length are padding: not read, output and
-                               gradients zero.  out_features = heads*head_dim, S = seq_len.  The values of rows that are not
+                               S each); rows of a sample at and behind its length are padding: their values have no effect
+                               (the stage's copy for the backward pass takes them along), their output and gradients are zero.
+                               out_features = heads*head_dim, S = seq_len.  The values of rows that are not
                                padding have to be finite: a key's NaN or infinity may reach queries that do not see it.
+                               Scores (scale * q . k) are held in fp32, for magnitudes below 2^16: beyond, the backward pass's
+                               probabilities are off by more than half a percent, and from 2^28 on results may not be finite.
                                head_dim up to 256, b * heads * ceil(S / 4) up to 2^23, b * kv_heads * ceil(S / 128) below 2^23.
                                A caller's tensor that either operator writes must not overlap one that it reads */
 } gpp_op_kind_t;
