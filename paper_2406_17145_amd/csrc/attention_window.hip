@@ -93,6 +93,7 @@ __global__ __launch_bounds__(256) void k_window_fwd(const WindowProb *__restrict
     const float v = w.row < len ? o[k] * inv : 0.0f;
     if (p.out) store_from_f32((void *)p.out, p.out_dtype, row * p.ld_out + (int64_t)w.h * p.dh + c, v);
     if (out2) store_from_f32((void *)out2, p.out_dtype, row * p.ld_ext + (int64_t)w.h * p.dh + c, v);
+    if (p.o_lo) store_from_f32((void *)p.o_lo, DT_BF16, row * p.ld_lo + (int64_t)w.h * p.dh + c, v - bf16_bits_to_f32(f32_to_bf16_bits(v)));
   }
   if (p.lse && lane == 0) p.lse[((int64_t)w.b * p.heads + w.h) * p.seq + w.row] = m + __builtin_amdgcn_logf(l);
 }
@@ -120,7 +121,8 @@ __global__ __launch_bounds__(256) void k_window_dq(const WindowProb *__restrict_
       qv[c] = load_as_f32((const void *)p.qkv, p.dtype, row * p.ld_qkv + (int64_t)w.h * p.dh + c);
       const float g = load_as_f32((const void *)dout, p.out_dtype, row * p.ld_dout + (int64_t)w.h * p.dh + c);
       gv[c] = g;
-      d += g * load_as_f32((const void *)p.o, p.out_dtype, row * p.ld_o + (int64_t)w.h * p.dh + c);
+      const float low = p.o_lo ? load_as_f32((const void *)p.o_lo, DT_BF16, row * p.ld_lo + (int64_t)w.h * p.dh + c) : 0.0f;
+      d += g * (load_as_f32((const void *)p.o, p.out_dtype, row * p.ld_o + (int64_t)w.h * p.dh + c) + low);
     }
     d = wave_sum(d);
     if (lane == 0) p.delta[stat] = d;

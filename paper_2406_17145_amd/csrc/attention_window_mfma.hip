@@ -13,9 +13,10 @@
 //   forward      S^T = K Q^T              O^T  += V^T P^T
 //   backward dQ  S^T = K Q^T, dP^T = V dO^T,  dQ^T += K^T dS^T
 //   backward dKV S   = Q K^T, dP   = dO V^T,  dV += P^T dO,  dK += dS^T Q
-// P and dS enter the second products in the storage type, as operands of the matrix cores; all sums are fp32.  In bf16 the gradients are
-// then off by 0.0024 (l2-relative), where rounding nothing but the results costs 0.0017; by up to 0.0031 in dQ and dK of samples of a few
-// tokens, where the rounding of O in rowsum(dO * O) weighs more.  No atomics: dQ has its own kernel, and sums over a long run of
+// P and dS enter the second products in the storage type, as operands of the matrix cores; all sums are fp32.  In bf16 the output is
+// then off by up to 0.0023 (l2-relative), the gradients by 0.0024 to 0.0025, where rounding nothing but the results costs 0.0017.  For
+// rowsum(dO * O) O is read back as it was rounded; where queries see few keys, whose score gradients are small differences, with what the
+// rounding took off (o_lo).  Peaked probabilities over many keys still show it: dQ and dK are off by 0.005 with scores spread by 8.  No atomics: dQ has its own kernel, and sums over a long run of
 // queries that are split over workgroups meet in a fixed order.
 //
 // What bounds it.  Long rows: matrix cores and vector unit (exponentials, masks, conversions) of a SIMD's two waves are busy half of the
@@ -277,7 +278,7 @@ __device__ __forceinline__ int win_spread(int idx, int total, const FastDiv &by)
 __device__ __forceinline__ void win_fetch(const WindowProb &p) {
   asm volatile("" ::"s"(p.qkv), "s"(p.out), "s"(p.o), "s"(p.dout), "s"(p.lse), "s"(p.delta), "s"(p.lengths), "s"(p.ld_qkv), "s"(p.ld_out), "s"(p.window),
                "s"(p.sinks), "s"(p.heads), "s"(p.kv_heads), "s"(p.seq), "s"(p.dh), "s"(p.causal), "s"(p.scale), "s"(p.ext_out), "s"(p.query_units),
-               "s"(p.units), "s"(p.whole), "s"(p.by_group.m), "s"(p.by_kv_heads.m), "s"(p.by_key_blocks.m));
+               "s"(p.units), "s"(p.whole), "s"(p.o_lo), "s"(p.ld_lo), "s"(p.by_group.m), "s"(p.by_kv_heads.m), "s"(p.by_key_blocks.m));
 }
 
 // Visible rows of a 32-row result as bits, shifted so that register r of the lane has bit 8 (r / 4) + r % 4; and a value kept where the
@@ -387,13 +388,14 @@ __device__ __forceinline__ WinBlock win_query_block(const WindowProb &p, int blk
 }
 
 // a wave's transposed result (rows: columns of the head, lane: its query) times `mul` of the lane through its own piece of LDS to rows;
-// rows at and behind `len` are written as zero
-template <typename T, int DH>
+// rows at and behind `len` are written as zero.  LOW: what the rounding took off the values, rounded in its turn, to rows in front of len
+template <typename T, int DH, bool LOW = false>
 __device__ __forceinline__ void win_store_rows(unsigned char *lds, int wave, const f32x16 (&acc)[DH / 32], float mul, int q0, int len, int seq,
                                                int dh, GPP_G void *out, int64_t row0, int64_t ld, GPP_G void *out2, int64_t ld2, int64_t col0) {
   constexpr int ST = DH * (int)sizeof(T) + 16, EPC = 16 / sizeof(T);
   unsigned char *stage = lds + wave * 32 * ST;
   const int l = threadIdx.x & 63;
+  if (LOW) seq = len;
 #pragma unroll
   for (int d = 0; d < DH / 32; ++d)
 #pragma unroll
@@ -401,8 +403,9 @@ __device__ __forceinline__ void win_store_rows(unsigned char *lds, int wave, con
       T v[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        if constexpr (sizeof(T) == 2) v[e] = f32_to_bf16_bits(acc[d][r + e] * mul);
-        else v[e] = acc[d][r + e] * mul;
+        const float x = acc[d][r + e] * mul;
+        if constexpr (sizeof(T) == 2) v[e] = f32_to_bf16_bits(LOW ? x - bf16_bits_to_f32(f32_to_bf16_bits(x)) : x);
+        else v[e] = x;
       }
       __builtin_memcpy(stage + (l & 31) * ST + (32 * d + win_acc_row(r)) * sizeof(T), v, sizeof(v));
     }
@@ -602,13 +605,20 @@ __global__ __launch_bounds__(256, 2) void k_window_fwd_mfma(const WindowProb *__
     if (p.lse && lane < 32 && q < len) p.lse[((int64_t)w.b * p.heads + w.h) * p.seq + q] = m + __builtin_amdgcn_logf(l);
     win_store_rows<T, DH>(lds, qg, o, 1.0f / l, q0, len, p.seq, p.dh, p.out, row0, p.ld_out, p.ext_out >= 0 ? (GPP_G void *)ext.p[p.ext_out] : nullptr,
                           p.ld_ext, (int64_t)w.h * p.dh);
+    if constexpr (sizeof(T) == 2) {
+      if (p.o_lo) {
+        __builtin_amdgcn_wave_barrier();
+        win_store_rows<T, DH, true>(lds, qg, o, 1.0f / l, q0, len, p.seq, p.dh, p.o_lo, row0, p.ld_lo, nullptr, 0, (int64_t)w.h * p.dh);
+      }
+    }
   }
   if (p.qkv_keep) keep.store(p, w, row0);
 }
 
 // ======================================================================= backward: dQ, and delta = rowsum(dO * O)
-// (`local`: block of queries of the record; `lds`: Q::LDS bytes.  DELTA: the deltas are written for the dK / dV kernel behind this one)
-template <typename T, int DH, int NW, int KG, bool DELTA>
+// (`local`: block of queries of the record; `lds`: Q::LDS bytes.  DELTA: the deltas are written for the dK / dV kernel behind this one.
+// LOW: the record may have a lower half of O)
+template <typename T, int DH, int NW, int KG, bool DELTA, bool LOW>
 __device__ __forceinline__ void win_dq_body(const WindowProb &p, const ExtPtrs &ext, int local, unsigned char *lds) {
   typedef WinTile<T, DH, KG> C;
   typedef WinFrag<T> F;
@@ -638,6 +648,13 @@ __device__ __forceinline__ void win_dq_body(const WindowProb &p, const ExtPtrs &
     const WinRows<T, DH> of = win_rows<T, DH>(p.o, row0 + qc, p.ld_o, (int64_t)w.h * p.dh, p.dh);
 #pragma unroll
     for (int s = 0; s < C::KS; ++s) delta = F::dot(gf.f[s], of.f[s], delta);
+    if constexpr (LOW) {
+      if (p.o_lo) {
+        const WinRows<T, DH> low = win_rows<T, DH>(p.o_lo, row0 + qc, p.ld_lo, (int64_t)w.h * p.dh, p.dh);
+#pragma unroll
+        for (int s = 0; s < C::KS; ++s) delta = F::dot(gf.f[s], low.f[s], delta);
+      }
+    }
     delta = win_half_sum(delta);
     if (DELTA && kg == 0 && lane < 32 && q < len) p.delta[stat] = -delta;      // (as the dK / dV kernel takes it)
   }
@@ -762,24 +779,28 @@ __device__ __forceinline__ WinSteps win_steps(const WindowProb &p, int c0, int l
 // registers each; with heads of more than 64 columns the sums take 128 of them, so V is then read from LDS like the tiles, K stays
 // in registers.
 // OWN: the deltas are formed here, from a tile of O beside the one of dO, instead of read from the dQ kernel in front of this one.
-template <typename T, int DH, bool OWN>
+// LOW: records may have a lower half of O, a fourth tile; where the LDS does not hold one per buffer, there is one, and all
+// waves have read it before the next is copied.
+template <typename T, int DH, bool OWN, bool LOW = false>
 struct WinKeyCfg {
   typedef WinTile<T, DH> C;
   static constexpr int QG = C::SUB, NW = 4 * QG;
-  static constexpr int STAT = (OWN ? 3 : 2) * C::BYTES, BUF = STAT + 1024;       // Q, dO (and O), the log-sum-exps and deltas of the tile's queries
+  static constexpr bool LOW_ONE = LOW && C::RB > 128;
+  static constexpr int STAT = (OWN ? 3 : 2) * C::BYTES + (LOW && !LOW_ONE ? C::BYTES : 0), BUF = STAT + 1024;       // Q, dO (and O), the log-sum-exps and deltas of the tile's queries
   static constexpr bool V_LDS = sizeof(T) == 2 && DH > 64;
   static constexpr int V_BYTES = V_LDS ? WIN_ROWS / C::RPG * C::GROUP : 0, ST = DH * C::ES + 16;
   static constexpr int JOIN = QG > 1 ? NW * 32 * DH * 4 : 0, OUT = NW * 32 * ST;    // over the tiles: a half of every wave's sums, rows of the result
   static constexpr int NB = C::RB == 128 ? 4 : (DH * C::ES > 256 || OWN ? 2 : 3);  // buffers, as many as the LDS of a compute unit's workgroups holds
   static constexpr int CP = (OWN ? 3 : 2) * C::KT / C::RPG / NW;                               // copies of a wave per step, at least
-  static constexpr int TILES = NB * BUF + V_BYTES + (OWN ? NW * 128 : 0), LDS = TILES > JOIN ? (TILES > OUT ? TILES : OUT) : (JOIN > OUT ? JOIN : OUT);
+  static constexpr int LOW_AT = LOW_ONE ? NB * BUF + V_BYTES + NW * 128 : 3 * C::BYTES;         // of a buffer, or of all
+  static constexpr int TILES = NB * BUF + V_BYTES + (OWN ? NW * 128 : 0) + (LOW_ONE ? C::BYTES : 0), LDS = TILES > JOIN ? (TILES > OUT ? TILES : OUT) : (JOIN > OUT ? JOIN : OUT);
 };
 
-template <typename T, int DH, bool OWN>
+template <typename T, int DH, bool OWN, bool LOW = false>
 __device__ __forceinline__ void win_dkv_body(const WindowProb &p, const ExtPtrs &ext, int local, unsigned char *lds) {
   typedef WinTile<T, DH> C;
   typedef WinFrag<T> F;
-  typedef WinKeyCfg<T, DH, OWN> K;
+  typedef WinKeyCfg<T, DH, OWN, LOW> K;
   GPP_G void *dqkv = p.ext_out >= 0 ? (GPP_G void *)ext.p[p.ext_out] : p.out;
   if (!dqkv) return;
   // (the unsplit units first, then the others)
@@ -799,16 +820,19 @@ __device__ __forceinline__ void win_dkv_body(const WindowProb &p, const ExtPtrs 
   const int64_t kcol = (int64_t)(p.heads + w.g) * p.dh, vcol = kcol + (int64_t)p.kv_heads * p.dh;
   const WinCopy<T, DH, K::NW> cq = win_copy_offsets<T, DH, K::NW>(wave, p.ld_qkv, p.dh), cg = win_copy_offsets<T, DH, K::NW>(wave, p.ld_dout, p.dh);
   const WinCopy<T, DH, K::NW> cw = win_copy_offsets<T, DH, K::NW>(wave, OWN ? p.ld_o : 0, p.dh);      // (O's)
+  const WinCopy<T, DH, K::NW> cl = win_copy_offsets<T, DH, K::NW>(wave, LOW ? p.ld_lo : 0, p.dh);
   const uint32_t lds0 = lds_address((const uint16_t *)lds);
   // of the next step to be copied: tile of its head, rows of the sample from there on, Q, dO, and (wave 0, 1) log-sum-exps or deltas
   int head = s0 < s1 ? s0 / nt : 0, tile = s0 - head * nt, rows = len - (t0 + tile) * C::KT;
   const GPP_G T *qn = qkv + (row0 + (t0 + tile) * C::KT) * p.ld_qkv + (int64_t)(h0 + head) * p.dh;
   const GPP_G T *gn = dout + (row0 + (t0 + tile) * C::KT) * p.ld_dout + (int64_t)(h0 + head) * p.dh;
   const GPP_G T *on = OWN ? (const GPP_G T *)p.o + (row0 + (t0 + tile) * C::KT) * p.ld_o + (int64_t)(h0 + head) * p.dh : nullptr;
+  const GPP_G T *ln = LOW && p.o_lo ? (const GPP_G T *)p.o_lo + (row0 + (t0 + tile) * C::KT) * p.ld_lo + (int64_t)(h0 + head) * p.dh : nullptr;
   const GPP_G float *sn = (wave == 0 ? p.lse : p.delta) + ((int64_t)w.b * p.heads + h0 + head) * p.seq + (t0 + tile) * C::KT;
   const int64_t q_step = C::KT * p.ld_qkv, g_step = C::KT * p.ld_dout;
   const uint32_t q_whole = win_tile_bytes(C::KT, p.ld_qkv, p.dh, C::ES), q_tail = win_tile_bytes((len - 1) % C::KT + 1, p.ld_qkv, p.dh, C::ES);
-  const int64_t o_step = C::KT * p.ld_o;
+  const int64_t o_step = C::KT * p.ld_o, l_step = C::KT * p.ld_lo;
+  const uint32_t l_whole = win_tile_bytes(C::KT, p.ld_lo, p.dh, C::ES), l_tail = win_tile_bytes((len - 1) % C::KT + 1, p.ld_lo, p.dh, C::ES);
   const uint32_t o_whole = win_tile_bytes(C::KT, p.ld_o, p.dh, C::ES), o_tail = win_tile_bytes((len - 1) % C::KT + 1, p.ld_o, p.dh, C::ES);
   const uint32_t g_whole = win_tile_bytes(C::KT, p.ld_dout, p.dh, C::ES), g_tail = win_tile_bytes((len - 1) % C::KT + 1, p.ld_dout, p.dh, C::ES);
   auto copy_next = [&](int buf) {
@@ -822,6 +846,14 @@ __device__ __forceinline__ void win_dkv_body(const WindowProb &p, const ExtPtrs 
       settle(ro, same);
       win_copy(ro, cw, lds0 + buf * K::BUF + 2 * C::BYTES, wave);
       on += o_step;
+    }
+    if constexpr (LOW) {
+      if (p.o_lo) {
+        rsrc4 rl = win_rsrc(ln, full ? l_whole : l_tail), same = rl;
+        settle(rl, same);
+        win_copy(rl, cl, lds0 + (K::LOW_ONE ? 0 : buf * K::BUF) + K::LOW_AT, wave);
+        ln += l_step;
+      }
     }
     if (wave < (OWN ? 1 : 2)) {      // (queries behind the end: zero, as their rows)
       rsrc4 rs = win_rsrc(sn, (uint32_t)min(rows, C::KT) * 4), same = rs;
@@ -837,6 +869,7 @@ __device__ __forceinline__ void win_dkv_body(const WindowProb &p, const ExtPtrs 
       qn += p.dh - nt * q_step;
       gn += p.dh - nt * g_step;
       if (OWN) on += p.dh - nt * o_step;
+      if (LOW) ln += p.dh - nt * l_step;
       sn += p.seq - nt * C::KT;
       rows += nt * C::KT;
     }
@@ -878,11 +911,21 @@ __device__ __forceinline__ void win_dkv_body(const WindowProb &p, const ExtPtrs 
   for (int s = s0; s < s1; ++s) {
     if (s + K::NB - 1 <= s1) copies_landed_barrier<(K::NB - 2) * K::CP>();
     else copies_landed_barrier<0>();
+    const unsigned char *tq = lds + out * K::BUF, *tg = tq + C::BYTES;
+    float own = 0.0f;
+    if constexpr (LOW) {
+      const unsigned char *low = K::LOW_ONE ? lds + K::LOW_AT : tq + K::LOW_AT;
+      if (p.o_lo) {
+#pragma unroll
+        for (int x = 0; x < C::KS; ++x)
+          own = F::dot(win_row_frag<T, DH>(at, tg + C::at(32) * qg, 0, x), win_row_frag<T, DH>(at, low + C::at(32) * qg, 0, x), own);
+        if (K::LOW_ONE) __syncthreads();      // read by all: the next tile may come
+      }
+    }
     if (s + K::NB - 1 < s1) {
       copy_next(in);
       in = in + 1 == K::NB ? 0 : in + 1;
     }
-    const unsigned char *tq = lds + out * K::BUF, *tg = tq + C::BYTES;
     out = out + 1 == K::NB ? 0 : out + 1;
     const int i0 = (t0 + now) * C::KT + 32 * qg;
     now = now + 1 == nt ? 0 : now + 1;
@@ -898,7 +941,6 @@ __device__ __forceinline__ void win_dkv_body(const WindowProb &p, const ExtPtrs 
         for (int e = 0; e < 4; ++e) dp[4 * k + e] = minus[e];
       }
     }
-    float own = 0.0f;
 #pragma unroll
     for (int x = 0; x < C::KS; ++x) {
       st = F::mma(win_row_frag<T, DH>(at, tq + C::at(32) * qg, 0, x), kf.f[x], st);
@@ -1014,18 +1056,18 @@ __global__ __launch_bounds__((WinKeyCfg<T, DH, false>::NW * 64), (DH * sizeof(T)
 
 // Small problems: dK / dV and dQ side by side in one launch, first the blocks of keys, then those of queries.  A launch of few
 // workgroups is as long as the chain of one of them, and together they still find a compute unit each.
-template <typename T, int DH>
+template <typename T, int DH, bool LOW>
 __global__ __launch_bounds__((WinKeyCfg<T, DH, true>::NW * 64), (DH * sizeof(T) <= 256 ? 2 : 1)) void k_window_bwd_mfma(const WindowProb *__restrict__ probs,
                                                                                                              int n, ExtPtrs ext) {
-  typedef WinKeyCfg<T, DH, true> K;
+  typedef WinKeyCfg<T, DH, true, LOW> K;
   typedef WinQueryCfg<T, DH, K::NW, 2> Q;
   __shared__ __attribute__((aligned(16))) unsigned char lds[K::LDS > Q::LDS ? K::LDS : Q::LDS];
   const int pi = find_prob(probs, n, blockIdx.x);
   const WindowProb p = probs[pi];
   win_fetch(p);
   const int local = blockIdx.x - p.blk_begin;
-  if (local < p.units) win_dkv_body<T, DH, true>(p, ext, local, lds);
-  else win_dq_body<T, DH, K::NW, 2, false>(p, ext, local - p.units, lds);
+  if (local < p.units) win_dkv_body<T, DH, true, LOW>(p, ext, local, lds);
+  else win_dq_body<T, DH, K::NW, 2, false, LOW>(p, ext, local - p.units, lds);
 }
 
 // The sums of a split block's parts, in order: four columns of a key per thread, DH / 4 workgroups per block (bound by memory; 12 us for
@@ -1084,7 +1126,7 @@ __global__ __launch_bounds__(256, 2) void k_window_dq_mfma(const WindowProb *__r
   const WindowProb p = probs[pi];
   win_fetch(p);
   const int local = blockIdx.x - p.blk_begin;
-  if (local < p.query_units) win_dq_body<T, DH, 4, KG, true>(p, ext, local, lds);
+  if (local < p.query_units) win_dq_body<T, DH, 4, KG, true, sizeof(T) == 2>(p, ext, local, lds);
   else win_join_body<T, DH>(p, ext, local - p.query_units);
 }
 
@@ -1249,9 +1291,11 @@ void launch_window_dkv_mfma(const WindowProb *probs, int n, int total_blocks, in
   WIN_INSTANCE(GO);
 #undef GO
 }
-void launch_window_bwd_mfma(const WindowProb *probs, int n, int total_blocks, int dtype, int dh, const ExtPtrs &ext, hipStream_t s) {
+void launch_window_bwd_mfma(const WindowProb *probs, int n, int total_blocks, int dtype, int dh, bool low, const ExtPtrs &ext, hipStream_t s) {
   if (total_blocks <= 0) return;
-#define GO(T, DH) hipLaunchKernelGGL((k_window_bwd_mfma<T, DH>), dim3(total_blocks), dim3((WinKeyCfg<T, DH, true>::NW * 64)), 0, s, probs, n, ext)
+#define GO(T, DH)                                                                                                         \
+  hipLaunchKernelGGL((low ? k_window_bwd_mfma<T, DH, sizeof(T) == 2> : k_window_bwd_mfma<T, DH, false>), dim3(total_blocks), \
+                     dim3((WinKeyCfg<T, DH, true>::NW * 64)), 0, s, probs, n, ext)
   WIN_INSTANCE(GO);
 #undef GO
 }

@@ -149,6 +149,8 @@ struct WindowProb {
   GPP_G int32_t *lengths_keep;    // fwd, or null: the lengths are copied here for the backward pass
   GPP_G void *qkv_keep;    // fwd, or null: the rows behind ext_qkv are copied here for the backward pass
   int64_t ld_keep;
+  GPP_G uint16_t *o_lo;    // or null: what rounding O to bf16 took off it, in bf16 (fwd writes it, bwd reads it for delta)
+  int64_t ld_lo;
   int64_t ld_qkv, ld_out, ld_o, ld_dout;
   int64_t window, sinks;   // window 0: S (no limit)
   int32_t batch, heads, kv_heads, seq, dh, causal;
@@ -391,7 +393,7 @@ int64_t window_partial_bytes(const WindowProb &p, int dh);
 void launch_window_fwd_mfma(const WindowProb *probs, int n, int total_blocks, int dtype, int dh, int key_groups, const ExtPtrs &ext, StageFlags *flags, hipStream_t s);
 void launch_window_dq_mfma(const WindowProb *probs, int n, int total_blocks, int dtype, int dh, int key_groups, const ExtPtrs &ext, hipStream_t s);
 void launch_window_dkv_mfma(const WindowProb *probs, int n, int total_blocks, int dtype, int dh, const ExtPtrs &ext, hipStream_t s);
-void launch_window_bwd_mfma(const WindowProb *probs, int n, int total_blocks, int dtype, int dh, const ExtPtrs &ext, hipStream_t s);
+void launch_window_bwd_mfma(const WindowProb *probs, int n, int total_blocks, int dtype, int dh, bool low, const ExtPtrs &ext, hipStream_t s);
 void launch_window_join(const WindowProb *probs, int n, int total_blocks, int dtype, int dh, const ExtPtrs &ext, hipStream_t s);
 int window_blocks(int64_t batch, int heads, int seq);
 

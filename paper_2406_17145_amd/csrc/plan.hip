@@ -21,6 +21,18 @@ static int64_t ld_of(int64_t features) { return align_up(features, 64); }
 static int64_t esize(int32_t dt) { return dt == DT_BF16 ? 2 : 4; }
 static bool is_float(int32_t dt) { return dt == DT_F32 || dt == DT_BF16; }
 
+// Whether a windowed attention in bf16 keeps what rounding took off its output, for rowsum(dO * O) in the backward pass: where a query
+// sees fewer than 48 keys on average.  Of few keys O is nearly one of the values, and dP - rowsum(dO * O) a small difference: dQ and dK are
+// off by 0.0025 (l2-relative) with the lower half and by 0.0031 (3 keys) to 0.0037 (2 keys) without, 0.0024 and 0.0028 with 16; with 50
+// keys 0.0024 and 0.0025.  It costs a tensor of O's size written and read: steps of 14 x 31, causal, 14.4 -> 16.0 us, 3 x 200, window 20, heads of
+// 96 26.8 -> 31.0, 1 x 16384, window 40 118 -> 135; where it is not kept, 4 x 512, window 128 would take 49.7 instead of 45.3.
+static bool window_keeps_low(const gpp_op_desc_t &d) {
+  const double seq = d.seq_len, near = d.window ? std::min<double>(d.window, seq) : seq;
+  double keys = d.causal ? near - near * (near - 1) / (2 * seq) : 2 * near - 1 - near * (near - 1) / seq;      // in the window
+  keys += std::min<double>(d.sinks, seq - near) * (1 - near / seq);                                            // about: first tokens in front of it
+  return keys > 1 && keys < 48;
+}
+
 #define FAIL(code, msg)      \
   do {                       \
     error = (msg);           \
@@ -482,6 +494,7 @@ gpp_status_t Plan::analyse(const gpp_stage_desc_t *desc) {
     if (d.kind == GPP_OP_ATTENTION_WINDOW && nd.wants_grad) {
       nd.stat0 = alloc(SP_SLOT, 1, micro_batch * d.heads * d.seq_len, DT_F32);    // log-sum-exp
       nd.stat1 = alloc(SP_SHARED, 1, micro_batch * d.heads * d.seq_len, DT_F32);  // rowsum(dO*O)
+      if (d.dtype == DT_BF16 && window_keeps_low(d)) nd.extra = alloc(SP_SLOT, nd.rows, nd.feat, DT_BF16);     // the lower half of O
     }
     if (d.kind == GPP_OP_EMBEDDING_BAG_SUM || d.kind == GPP_OP_EMBEDDING_BAG_CONCAT) {
       const int64_t cap = micro_batch * d.bag_size;
@@ -788,6 +801,8 @@ struct Emitter {
     a.out_dtype = d.dtype;
     a.ext_qkv = a.ext_out = a.ext_dout = a.ext_len = -1;
     if (nd.in.size() == 2) a.lengths = (const int32_t *)ptr(pl.nodes[nd.in[1]].val);
+    a.o_lo = (uint16_t *)ptr(nd.extra);
+    a.ld_lo = nd.extra.ld;
     return a;
   }
 
@@ -795,12 +810,13 @@ struct Emitter {
   // head dimension; 0: the row-parallel kernels
   void emit_windows(std::vector<WindowProb> &recs, bool backward) {
     auto mfma_dh = [&](const WindowProb &a) { return (pl.flags & 1) || (backward && a.grad_dtype != a.dtype) ? 0 : window_mfma_dh(a); };
-    auto step = [&](int kern, std::vector<WindowProb> &now, int dtype, int dh, int groups, auto blocks_of) {
+    // (`form`: the waves that share 32 queries; of the kernel that takes dQ and dK and dV whether a record has a lower half of O)
+    auto step = [&](int kern, std::vector<WindowProb> &now, int dtype, int dh, int form, auto blocks_of) {
       add_launches(kern, now, blocks_of, [&](Step &s) {
         s.ext_kind = EXT_BOTH;
         s.a0 = dtype;
         s.a1 = dh;
-        s.a2 = groups;
+        s.a2 = form;
       });
     };
     for (int32_t dt : {DT_F32, DT_BF16})
@@ -856,13 +872,14 @@ struct Emitter {
           pl.bwd_shared = true;
         }
         part_need = std::max(part_need, part_off);
+        const bool low = std::any_of(now.begin(), now.end(), [](const WindowProb &a) { return a.o_lo != nullptr; });
         if (one) {
-          step(K_WINDOW_BWD, now, dt, dh, 1, [&](const WindowProb &a) { return a.units + a.query_units; });
+          step(K_WINDOW_BWD, now, dt, dh, low, [&](const WindowProb &a) { return a.units + a.query_units; });
           step(K_WINDOW_JOIN, now, dt, dh, 1, [&](const WindowProb &a) { return window_join_blocks(a, dh); });
           continue;
         }
         if (joins > 0 && window_keys_first(dt, dh, blocks128)) {
-          step(K_WINDOW_BWD, now, dt, dh, 1, [&](const WindowProb &a) { return a.units; });
+          step(K_WINDOW_BWD, now, dt, dh, low, [&](const WindowProb &a) { return a.units; });
           step(K_WINDOW_DQ, now, dt, dh, groups, [&](const WindowProb &a) { return a.query_units + window_join_blocks(a, dh); });
           continue;
         }

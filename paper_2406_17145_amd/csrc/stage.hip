@@ -551,7 +551,7 @@ static gpp_status_t run_steps(gpp_stage *st, const std::vector<Step> &steps, int
         if (sp.a1) launch_window_dkv_mfma((const WindowProb *)tab, sp.n, sp.blocks, sp.a0, sp.a1, ext, s);
         else launch_window_dkv((const WindowProb *)tab, sp.n, sp.blocks, ext, s);
         break;
-      case K_WINDOW_BWD: launch_window_bwd_mfma((const WindowProb *)tab, sp.n, sp.blocks, sp.a0, sp.a1, ext, s); break;
+      case K_WINDOW_BWD: launch_window_bwd_mfma((const WindowProb *)tab, sp.n, sp.blocks, sp.a0, sp.a1, sp.a2 != 0, ext, s); break;
       case K_WINDOW_JOIN: launch_window_join((const WindowProb *)tab, sp.n, sp.blocks, sp.a0, sp.a1, ext, s); break;
       case K_POOL: launch_pool((const PoolProb *)tab, sp.n, sp.blocks, s); break;
       case K_EMB_FWD: launch_emb_fwd((const EmbProb *)tab, sp.n, sp.blocks, sp.a0, sp.a1, flags, s); break;

@@ -98,3 +98,20 @@ def test_memory_of_cut_sums_is_bounded(lib, dtype, causal, window, sinks, b, seq
     gradient = b * seq * (heads + 2 * kv) * dh * (2 if dtype == "bf16" else 4)
     ops = S.attention_ops(b, seq, heads, kv, dh, window=window, sinks=sinks, causal=causal, dtype=dtype)
     assert cut_sums(ops, b) <= max(64 << 20, 2 * gradient) + (1 << 20)
+
+
+@pytest.mark.parametrize("causal,window,sinks,kept", [(True, 40, 0, True), (True, 60, 0, False), (False, 20, 0, True), (False, 30, 0, False), (True, 20, 20, True),
+                                                      (True, 20, 40, False), (True, 1, 0, False), (False, 1, 0, False), (False, 1, 1, True), (True, 0, 0, False)])
+def test_lower_half_of_the_output_is_kept_for_few_keys(lib, causal, window, sinks, kept):
+    """In bf16; fp32 has none."""
+    seq, heads, kv, dh = 16384, 8, 8, 64
+    size = seq * heads * dh * 2
+    for dtype in ("bf16", "f32"):
+        ops = S.attention_ops(1, seq, heads, kv, dh, window=window, sinks=sinks, causal=causal, dtype=dtype)
+        d, keep = B.build_desc(ops, 1)
+        used = sum(s["kernel"] == "attention_bwd_dkv" for s in B.gpp_stage_describe(d)) > 1        # (cut sums beside it)
+        extra = cut_sums(ops, 1)
+        if not used:
+            assert abs(extra - (size if kept and dtype == "bf16" else 0)) < 64 << 10
+        else:
+            assert extra >= (size if kept and dtype == "bf16" else 0)
