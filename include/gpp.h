@@ -502,7 +502,9 @@ gpp_status_t gpp_stage_embedding_sort_result(gpp_stage_t *stage, int32_t op, con
  * allocation these calls ever make, and only in this mode).  profile_read waits for the recorded
  * events and returns, per tag, the accumulated milliseconds and kernel launches since the last
  * reset; ms and launches are HOST arrays of GPP_PROFILE_TAGS entries.  The tags gemm_skinny_fwd and gemm_skinny_dx hold
- * the launches of the few-row family on either of its kernels (gpp_stage_describe tells them apart).  enable = R > 1 (at most 64) is a
+ * the launches of the few-row family on either of its kernels (gpp_stage_describe tells them apart); elt_fwd and elt_bwd
+ * hold rotary positions too, the attention tags windowed attention (attention_bwd_dkv also the launches that take dQ beside dK and
+ * dV and those that join cut sums).  enable = R > 1 (at most 64) is a
  * TIMING-ONLY mode: every grouped GEMM launch is issued R times back to back inside its bracket, so that the
  * bracket's own dispatch latency (about two microseconds) is spread over R launches; accumulated gradients
  * and in-place sums of such a pass are meaningless. */
