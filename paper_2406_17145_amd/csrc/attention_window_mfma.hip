@@ -22,8 +22,8 @@
 // What bounds it.  Long rows: matrix cores and vector unit (exponentials, masks, conversions) of a SIMD's two waves are busy half of the
 // time each, and the clock falls under the load.  1 x 16384, window 4096, causal, 16 heads of 128 over 2, bf16: forward 572 us
 // (0.84 PFLOP/s of visible pairs, matrix cores busy 52 %), dQ 731 - 744 (0.98, 59 %), dK and dV 1036 - 1104 (0.9, 55 %), joining 12.  Heads of
-// 64: twice the vector work per product; 2 x 8192, window 1024, causal, 16 heads over 4: a step of 407 us, 0.71 PFLOP/s where
-// heads of 128 reach 0.98.  Short rows: a wave's chain through a tile, some 2000 cycles, between a launch's first loads and last stores;
+// 64: twice the vector work per product, and bank conflicts; 2 x 8192, window 1024, causal, 16 heads over 4: a step of 407 us, 0.71 PFLOP/s
+// where heads of 128 reach 0.98, matrix cores busy 34 to 45 %.  Short rows: a wave's chain through a tile, some 2000 cycles, between a launch's first loads and last stores;
 // 4 x 512, window 128, 16 heads of 64 over 4: forward 13 - 14 us, dK and dV 20, dQ and the joining 13.
 #include <algorithm>
 
