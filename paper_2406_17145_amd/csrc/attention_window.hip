@@ -6,7 +6,8 @@
 // (dK and dV summed over the query heads that share the key / value head).  One wavefront per query row (forward, dQ) or per
 // key row (dK, dV); the running maximum and sum of the softmax go over 64 keys at a time.  Deterministic: no atomics.
 // For what the matrix-core kernels (attention_window_mfma.hip) do not take: head dimensions above 128 or off 16 bytes, operands of two
-// storage types, an output in a merge at a column off 16 bytes.  Bound by the loads of a key's row per lane: 4 x 512, window 128, 16 heads of 64 in bf16 take 5.1 ms a step here, 45 us there.
+// storage types, an output in a merge at a column off 16 bytes.  Bound by the loads of a key's row per lane: 4 x 512, window 128, 16
+// heads of 64 in bf16 take 5.1 ms a step here, 45 us there.
 #include "device_utils.h"
 #include "window_utils.h"
 

@@ -16,15 +16,15 @@
 // P and dS enter the second products in the storage type, as operands of the matrix cores; all sums are fp32.  In bf16 the output is
 // then off by up to 0.0023 (l2-relative), the gradients by 0.0024 to 0.0025, where rounding nothing but the results costs 0.0017.  For
 // rowsum(dO * O) O is read back as it was rounded; where queries see few keys, whose score gradients are small differences, with what the
-// rounding took off (o_lo).  Peaked probabilities over many keys still show it: dQ and dK are off by 0.005 with scores spread by 8.  No atomics: dQ has its own kernel, and sums over a long run of
-// queries that are split over workgroups meet in a fixed order.
+// rounding took off (o_lo).  Peaked probabilities over many keys still show it: dQ and dK are off by 0.005 with scores spread by 8.
+// No atomics: dQ has its own kernel, and sums over a long run of queries that are split over workgroups meet in a fixed order.
 //
 // What bounds it.  Long rows: matrix cores and vector unit (exponentials, masks, conversions) of a SIMD's two waves are busy half of the
 // time each, and the clock falls under the load.  1 x 16384, window 4096, causal, 16 heads of 128 over 2, bf16: forward 572 us
 // (0.84 PFLOP/s of visible pairs, matrix cores busy 52 %), dQ 731 - 744 (0.98, 59 %), dK and dV 1036 - 1104 (0.9, 55 %), joining 12.  Heads of
 // 64: twice the vector work per product, and bank conflicts; 2 x 8192, window 1024, causal, 16 heads over 4: a step of 407 us, 0.71 PFLOP/s
-// where heads of 128 reach 0.98, matrix cores busy 34 to 45 %.  Short rows: a wave's chain through a tile, some 2000 cycles, between a launch's first loads and last stores;
-// 4 x 512, window 128, 16 heads of 64 over 4: forward 13 - 14 us, dK and dV 20, dQ and the joining 13.
+// where heads of 128 reach 0.98, matrix cores busy 34 to 45 %.  Short rows: a wave's chain through a tile, some 2000 cycles, between a
+// launch's first loads and last stores; 4 x 512, window 128, 16 heads of 64 over 4: forward 13 - 14 us, dK and dV 20, dQ and the joining 13.
 #include <algorithm>
 
 #include "gemm_direct.h"
@@ -43,7 +43,7 @@ constexpr int WIN_ROWS = 128;     // rows that a workgroup owns
 // of 16 consecutive rows (the swizzle spreads the rows of a group over the quarters of a line, the padding moves group after
 // group on by a chunk); across rows, the transposing read takes 64 bytes of each of four consecutive rows (each row another
 // quarter).  Measured, conflicts are 0 to 4 % of the LDS's active cycles with heads of 128 in bf16 and in fp32, 2 to 20 % with heads of 96,
-// and with rows of 128 bytes (heads of 64: 4 x 512 and 2 x 8192 alike) 24 to 40 %: there the lanes served together are others.
+// and with rows of 128 bytes (heads of 64: 4 x 512 and 2 x 8192 alike) 24 to 40 %: there it serves other lanes together.
 // A swizzle alone would do, but one that touches more bits of c costs every read of a row an address of its own.
 template <int RB>
 __device__ __forceinline__ int win_swizzle(int row) {

@@ -226,6 +226,19 @@ def test_more_inputs_and_outputs_than_a_launch_has_pointers_for():
     g.compare(b, feeds, 3)
 
 
+@pytest.mark.parametrize("dh", [32, 64, 96, 128])
+@pytest.mark.parametrize("b,seq", [(2, 150), (24, 400)])
+def test_branches_that_see_few_keys_and_many_share_a_launch(b, seq, dh):
+    """Of one launch's branches some keep the lower half of their output and some do not; one backward launch for all, or several."""
+    g, rng, feeds = Graph(seq), np.random.default_rng(38), {}
+    for window, causal in ((3, True), (0, True), (5, False), (90, False)):
+        x = g.input(4 * dh)
+        feeds[x] = W.round_to_bf16(rng.standard_normal((b * seq, 4 * dh)))
+        g.attention(x, 2, 1, dh, window=window, causal=causal)
+    # an attention
+    g.compare(b, feeds, 3, blocks={x: [slice(0, 2 * dh), slice(2 * dh, 3 * dh), slice(3 * dh, None)] for x in feeds})
+
+
 def test_branches_of_more_threads_than_a_launch_has():
     """Three attentions on a million single tokens each, in launches of their own: a token sees itself, so its output is V, dV is dO and
     the rest of the gradient is zero.  Then rotary positions of 2^27 rows."""
